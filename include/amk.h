@@ -283,6 +283,140 @@ int amk_trace_copy(amk_handle_t h, uint64_t* dst, int64_t capacity, int32_t* n_t
  * AMK_ERR_DEVICE for a launch failure. */
 int amk_read_probe(const void* buf, int64_t bytes, int32_t blocks, uint32_t* sink, void* stream);
 
+/* ---- operators for several tokens --------------------------------------------
+ *
+ * The decode step takes one token; these take many: the products with the
+ * decoder's weights, the attention of whole prompts and of drafted tokens over
+ * a KV cache, the log probabilities of given tokens, and moving accepted rows
+ * of a cache together.  amk_extend below runs the whole decoder with them.
+ *
+ * Common rules: every call enqueues on `stream` and returns at once; it
+ * allocates nothing and waits for nothing, so it may be captured into a graph
+ * (arguments read from HOST memory are read during the call; a replay repeats
+ * them).  Pointers are device memory of the current device, which is also the
+ * stream's, unless marked HOST.  Strides count elements.  Outputs are written
+ * only where a result is defined and never overlap inputs, except where said.
+ * A workspace is scratch memory of the call, 256-byte aligned: calls that may
+ * run at the same time (two streams, two graphs) need workspaces of their own.
+ * Errors are found before anything is launched: AMK_ERR_INVALID_ARGUMENT for a
+ * NULL or misaligned pointer, a size or stride out of range or a workspace too
+ * small, AMK_ERR_UNSUPPORTED for a shape outside the family, AMK_ERR_DEVICE for
+ * a failed launch.  Results do not depend on the order in which work happens to
+ * run: the same call gives the same bits. */
+
+/* Element types of operators that take several. */
+enum { AMK_F32 = 0, AMK_BF16 = 1, AMK_F16 = 2 };
+
+/* y = x W^T (accumulate 0) or y += x W^T (accumulate 1) for n tokens.
+ *   x: bf16 [n][in], rows x_stride apart (x and x_stride * 2 bytes 16-byte aligned)
+ *   w, scale: W [out][in] in weight_format, as under amk_linear_t (group_size as in
+ *             amk_config_t); in is a multiple of 16, under W4A16 of 32 and of the group
+ *   y: fp32 (y_type AMK_F32) or bf16 (AMK_BF16) [n][out], rows y_stride >= out apart
+ * Products are exact in fp32 and summed in fp32; a scale multiplies the fp32 sum
+ * of its row (W8A16) or group (W4A16).  n or out of 0 is a no-op. */
+int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t out, const void* w,
+               const void* scale, int32_t weight_format, int32_t group_size, void* y, int64_t y_stride,
+               int32_t y_type, int32_t accumulate, void* stream);
+
+/* Operands of an attention: bf16 q and out [token][n_heads][head_dim], k and v
+ * [row][n_kv_heads][head_dim], each element (t, h, i) at t * token stride +
+ * h * head stride + i.  Strides are positive multiples of 8, pointers 16-byte aligned.  One
+ * layer of the decoder's cache has k_token = head_dim and k_head = max_seq *
+ * head_dim.  n_heads is a multiple of n_kv_heads; query head h reads KV head
+ * h / (n_heads / n_kv_heads).  head_dim is 64 or 128; scale (positive,
+ * finite) multiplies the scores, usually 1 / sqrt(head_dim).
+ * Scores, softmax statistics and the weighted sums are fp32; weights are
+ * rounded to bf16 for the product with v.  A row that sees no key, or only keys
+ * scoring minus infinity, gets zeros; what a row does not see never reaches it,
+ * infinities and NaN included. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  int32_t n_heads, n_kv_heads, head_dim;
+  float scale;
+} amk_attention_t;
+
+/* Causal attention over whole prompts, n_seqs packed sequences: sequence b has
+ * the queries [cu_q[b], cu_q[b + 1]) of total_q and the keys [cu_k[b],
+ * cu_k[b + 1]) of total_k (device int32 [n_seqs + 1], not decreasing; offsets
+ * outside [0, total] are cut to it).  The last query is at the last key's
+ * position: query i of nq sees the keys up to nk - nq + i of nk (keys before
+ * the queries are an earlier context; with fewer keys than queries the first
+ * queries see none).  cu_q and cu_k NULL: one sequence (n_seqs 1) of total_q
+ * queries and total_k keys.  Rows of out outside every sequence stay as they
+ * were. */
+int amk_prompt_attention(const amk_attention_t* a, const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
+                         int32_t total_q, int32_t total_k, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace the call needs (0: none, the pointer may be NULL). */
+size_t amk_prompt_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
+                                      int32_t total_q, int32_t total_k);
+
+/* Most tokens of one tree. */
+#define AMK_TREE_MAX 64
+
+/* Attention of n drafted tokens (at most AMK_TREE_MAX) over a cache: token i
+ * sees the rows 0 .. pos - 1 of k and v and, of the rows pos .. pos + n - 1,
+ * row pos + j where bit j of masks[i] (HOST uint64 [n]) is set; bits n and up
+ * are ignored.  A chain of tokens has masks[i] = 2^(i + 1) - 1, a single one 1. */
+int amk_tree_attention(const amk_attention_t* a, int32_t n, int32_t pos, const uint64_t* masks, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+size_t amk_tree_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n, int32_t pos);
+
+/* Most alternatives amk_token_logprobs gives. */
+#define AMK_TOP_MAX 32
+
+/* For each of n rows of logits [n][vocab] (type AMK_F32, _BF16 or _F16, rows
+ * row_stride apart, aligned to the type):
+ *   logprob[i]: log softmax of the row at tokens[i] (int32 [n]; NaN for a token
+ *               outside [0, vocab))
+ *   entropy[i]: -sum p log p in nats, impossible tokens adding nothing
+ *   top_ids, top_logprobs [n][top]: the top (0 .. AMK_TOP_MAX, at most vocab)
+ *               most probable tokens, the lowest index first among equal logits
+ * tokens and logprob, and entropy, may be NULL.  A row that has no softmax (a
+ * NaN, plus infinity, or only minus infinities) gets NaN, its top_ids -1.
+ * vocab is at most 2^20; n = 0 is a no-op. */
+int amk_token_logprobs(const void* logits, int32_t type, int64_t row_stride, int32_t n, int32_t vocab,
+                       const int32_t* tokens, int32_t top, float* logprob, float* entropy, int32_t* top_ids,
+                       float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t amk_token_logprobs_workspace(int32_t type, int32_t n, int32_t vocab, int32_t top);
+
+/* In every layer and head of a KV cache (laid out as for amk_decode_step, head_dim
+ * 64 or 128), row pos + i takes the contents row pos + rows[i] had before the
+ * call, i < count <= AMK_TREE_MAX.  rows (HOST) ascend strictly from >= 0, so
+ * accepted tokens of a drafted tree move up to follow each other; rows past
+ * pos + count - 1 keep what they held.  16-byte aligned cache. */
+int amk_kv_keep(void* kv_cache, int32_t n_layers, int32_t n_kv_heads, int32_t max_seq, int32_t head_dim, int32_t pos,
+                const int32_t* rows, int32_t count, void* stream);
+
+/* Run n tokens through the handle's decoder behind the pos positions already in
+ * kv_cache: appends their K and V rows at pos .. pos + n - 1 of every layer and
+ * writes the logits of the last n_logits tokens (0 .. n) to logits
+ * [n_logits][vocab] (fp32, 16-byte aligned; may be NULL for n_logits 0).
+ *   tokens:  HOST int32 [n], each in [0, vocab); pos + n <= max_seq
+ *   parents: NULL for a chain (a prompt or part of one); or HOST int32 [n], n <=
+ *            AMK_TREE_MAX, a drafted tree: parents[i] in [-1, i) is the token that
+ *            token i follows, -1 the last position before pos.  Token i then sits
+ *            at the position of its depth (RoPE), in cache row pos + i, and sees
+ *            the earlier positions, its ancestors and itself; amk_kv_keep moves an
+ *            accepted branch together.
+ * kv_cache as for amk_decode_step.  The residual stream, norms, RoPE and softmax
+ * are fp32; the inputs of the products and attentions are rounded to bf16, which
+ * the decode step does not do, so logits differ from its by those roundings.
+ * The handle is only read and may be in use by steps on other streams; its
+ * sticky errors are not looked at or set.  Pointers are checked as in
+ * amk_decode_step. */
+int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, const int32_t* parents, void* kv_cache,
+               float* logits, int32_t n_logits, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace amk_extend needs for n tokens (0 for a NULL handle or n < 1). */
+size_t amk_extend_workspace(amk_handle_t h, int32_t n);
+
 /* ---- schedule introspection (CPU only, no device needed) -------------------- */
 
 /* Schedule variants.  All compute the same step; they differ in where the

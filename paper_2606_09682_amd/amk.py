@@ -34,6 +34,9 @@ AMK_WEIGHTS_W4A16 = 2
 AMK_SCHEDULE_SHORT, AMK_SCHEDULE_LONG, AMK_SCHEDULE_TINY = 0, 1, 2
 AMK_ASSIGN_ROUND_ROBIN, AMK_ASSIGN_LPT = 0, 1
 AMK_TINY_MAX = 8
+AMK_F32, AMK_BF16, AMK_F16 = 0, 1, 2
+AMK_TREE_MAX = 64
+AMK_TOP_MAX = 32
 AMK_OP_QKV, AMK_OP_ATTN, AMK_OP_COMBINE, AMK_OP_O, AMK_OP_GATEUP, AMK_OP_DOWN, AMK_OP_LMHEAD, AMK_OP_ARGMAX = range(1, 9)
 AMK_MAX_WAITS = 4
 AMK_CU_INLINE = -1
@@ -89,6 +92,14 @@ class amk_check_report_t(ctypes.Structure):
                 ("message", ctypes.c_char * 256)]
 
 
+class amk_attention_t(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "out_token",
+                                      "out_head")] + [
+        ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("scale", ctypes.c_float)]
+
+
 class AmkError(RuntimeError):
     def __init__(self, status: int, what: str = ""):
         self.status = status
@@ -134,6 +145,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "amk_trace_copy": (ctypes.c_int, [ctypes.c_void_p, P(ctypes.c_uint64), ctypes.c_int64, P(ctypes.c_int32),
                                           P(ctypes.c_int32)]),
     }
+    i32, i64, ptr, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
+    sig.update({
+        "amk_linear": (ctypes.c_int, [ptr, i64, i32, i32, i32, ptr, ptr, i32, i32, ptr, i64, i32, i32, ptr]),
+        "amk_prompt_attention": (ctypes.c_int, [P(amk_attention_t), ptr, ptr, i32, i32, i32, ptr, size, ptr]),
+        "amk_prompt_attention_workspace": (size, [i32] * 6),
+        "amk_tree_attention": (ctypes.c_int, [P(amk_attention_t), i32, i32, P(ctypes.c_uint64), ptr, size, ptr]),
+        "amk_tree_attention_workspace": (size, [i32] * 5),
+        "amk_token_logprobs": (ctypes.c_int, [ptr, i32, i64, i32, i32, ptr, i32, ptr, ptr, ptr, ptr, ptr, size, ptr]),
+        "amk_token_logprobs_workspace": (size, [i32] * 4),
+        "amk_kv_keep": (ctypes.c_int, [ptr, i32, i32, i32, i32, i32, P(i32), i32, ptr]),
+        "amk_extend": (ctypes.c_int, [ptr, P(i32), i32, i32, P(i32), ptr, ptr, i32, ptr, size, ptr]),
+        "amk_extend_workspace": (size, [ptr, i32]),
+    })
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype = res
@@ -240,6 +264,233 @@ def amk_schedule_check(cfg: amk_config_t, n_cu: int, tasks, n_counters: int,
     _check(load().amk_schedule_check(ctypes.byref(cfg), ctypes.byref(tuning) if tuning else None, n_cu, tasks,
                                      len(tasks), n_counters, ctypes.byref(rep)), "amk_schedule_check")
     return rep
+
+
+# ---- operators for several tokens over torch device tensors ---------------------------
+# Each call runs on the tensors' device and torch's current stream there, on which its
+# outputs and workspaces are allocated too; nothing synchronises.  The library sees
+# bare pointers, so types, shapes, devices and strides are checked here.
+_FORMATS = {"bf16": AMK_WEIGHTS_BF16, "w8a16": AMK_WEIGHTS_W8A16, "w4a16": AMK_WEIGHTS_W4A16}
+
+
+def _tensor(t, what: str, device, dtypes, dim: int):
+    """Check one operand: a tensor of `dim` dimensions and one of `dtypes` on `device`."""
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, expected {device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} has type {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if t.dim() != dim:
+        raise ValueError(f"{what} has {t.dim()} dimensions, expected {dim}")
+    return t
+
+
+def _cuda(t, what: str):
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    return t.device
+
+
+def _stream(device) -> int:
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _call(device, fn, *args) -> None:
+    """Run fn(*args) with `device` current and raise on an error status."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args)
+    if status != AMK_OK:
+        raise AmkError(status, fn.__name__)
+
+
+def _workspace(nbytes: int, device):
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, out=None, out_dtype=None,
+           accumulate: bool = False):
+    """x W^T for n tokens (amk_linear): x bf16 [n, in] with contiguous rows; w and
+    scale a projection as Decoder takes it ([out, in] bf16 or int16 bits; int8 with
+    fp32 scale [out]; packed uint8 [out, in / 2] with fp16 scale [out, in / group]).
+    Returns [n, out] of out_dtype (fp32, the default, or bf16), or writes it to `out`
+    (contiguous rows) and returns that; accumulate adds to `out`."""
+    import torch
+    if weight_format not in _FORMATS:
+        raise ValueError(f"unknown weight format {weight_format}")
+    fmt = _FORMATS[weight_format]
+    device = _cuda(x, "x")
+    _tensor(x, "x", device, (torch.bfloat16, torch.int16), 2)
+    n, width = x.shape
+    if n and x.stride(1) != 1:
+        raise ValueError("x must have contiguous rows")
+    w_types = {AMK_WEIGHTS_BF16: (torch.bfloat16, torch.int16), AMK_WEIGHTS_W8A16: (torch.int8,),
+               AMK_WEIGHTS_W4A16: (torch.uint8,)}[fmt]
+    _tensor(w, "w", device, w_types, 2)
+    rows = w.shape[0]
+    if not w.is_contiguous() or w.shape[1] * (2 if fmt == AMK_WEIGHTS_W4A16 else 1) != width:
+        raise ValueError(f"w must be contiguous rows of {width} columns")
+    scale_ptr = None
+    if fmt != AMK_WEIGHTS_BF16:
+        if scale is None:
+            raise ValueError(f"{weight_format} weights need a scale")
+        w4 = fmt == AMK_WEIGHTS_W4A16
+        _tensor(scale, "scale", device, (torch.float16,) if w4 else (torch.float32,), 2 if w4 else 1)
+        if not scale.is_contiguous() or scale.numel() != (rows * (width // (group_size or 128)) if w4 else rows):
+            raise ValueError("scale must be contiguous, one value per row (and group of columns)")
+        scale_ptr = scale.data_ptr()
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty(n, rows, dtype=out_dtype or torch.float32, device=device)
+    _tensor(out, "out", device, (torch.float32, torch.bfloat16) if out_dtype is None else (out_dtype,), 2)
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be float32 or bfloat16")
+    if tuple(out.shape) != (n, rows) or (out.numel() and out.stride(1) != 1):
+        raise ValueError(f"out must be [{n}, {rows}] with contiguous rows")
+    _call(device, load().amk_linear, x.data_ptr(), x.stride(0) if n > 1 else (width + 7) // 8 * 8, n, width, rows,
+          w.data_ptr(), scale_ptr, fmt, group_size, out.data_ptr(), out.stride(0) if n > 1 else rows,
+          AMK_F32 if out.dtype == torch.float32 else AMK_BF16, int(accumulate), _stream(device))
+    return out
+
+
+def _attention(q, k, v, scale, out):
+    """(amk_attention_t, out) of operands [tokens, heads, head_dim] after checking them."""
+    import torch
+    device = _cuda(q, "q")
+    bf16 = (torch.bfloat16, torch.int16)
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        _tensor(t, what, device, bf16, 3)
+    tokens, heads, d = q.shape
+    rows, kv_heads, _ = k.shape
+    if k.shape != v.shape or k.shape[2] != d:
+        raise ValueError("k and v must be [rows, kv heads, head_dim] with q's head_dim")
+    if out is None:
+        out = torch.empty(tokens, heads, d, dtype=q.dtype, device=device)
+    else:
+        _tensor(out, "out", device, bf16, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    a = amk_attention_t()
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        token, head, one = t.stride()
+        if t.numel() and one != 1 and d > 1:
+            raise ValueError(f"{name} must have contiguous heads")
+        setattr(a, name, t.data_ptr() or None)
+        # a dimension of one element is not stepped over: any stride will do
+        setattr(a, name + "_token", token if t.shape[0] > 1 else 8)
+        setattr(a, name + "_head", head if t.shape[1] > 1 else 8)
+    a.n_heads, a.n_kv_heads, a.head_dim = heads, kv_heads, d
+    a.scale = 1.0 / d ** 0.5 if scale is None else scale
+    return a, out, device
+
+
+def prompt_attention(q, k, v, cu_q=None, cu_k=None, scale: Optional[float] = None, out=None):
+    """Causal attention over whole prompts (amk_prompt_attention): q bf16 [tokens,
+    heads, head_dim], k and v [rows, kv heads, head_dim], any strides with contiguous
+    heads (a cache layer kv[l, 0] is taken as kv[l, 0].transpose(0, 1)).  cu_q and
+    cu_k: int32 device tensors [sequences + 1] of offsets, or both None for one
+    sequence.  Rows of `out` outside every sequence are not written."""
+    import torch
+    a, out, device = _attention(q, k, v, scale, out)
+    seqs, pq, pk = 1, None, None
+    if (cu_q is None) != (cu_k is None):
+        raise ValueError("cu_q and cu_k come together")
+    if cu_q is not None:
+        for t, what in ((cu_q, "cu_q"), (cu_k, "cu_k")):
+            _tensor(t, what, device, (torch.int32,), 1)
+            if not t.is_contiguous() or t.numel() != cu_q.numel() or t.numel() < 1:
+                raise ValueError("cu_q and cu_k must be contiguous and of one length")
+        seqs, pq, pk = cu_q.numel() - 1, cu_q.data_ptr(), cu_k.data_ptr()
+    lib = load()
+    tokens, rows = q.shape[0], k.shape[0]
+    need = lib.amk_prompt_attention_workspace(a.n_heads, a.n_kv_heads, a.head_dim, seqs, tokens, rows)
+    ws = _workspace(need, device)
+    _call(device, lib.amk_prompt_attention, a, pq, pk, seqs, tokens, rows, ws.data_ptr() if need else None, need,
+          _stream(device))
+    return out
+
+
+def tree_masks(parents):
+    """The masks of a drafted tree: token i sees its ancestors and itself
+    (parents[i] in [-1, i), -1 for a token that follows the context)."""
+    masks = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise ValueError(f"parents[{i}] = {p} is not in [-1, {i})")
+        masks.append(1 << i | (masks[p] if p >= 0 else 0))
+    return masks
+
+
+def tree_attention(q, k, v, pos: int, masks, scale: Optional[float] = None, out=None):
+    """Attention of n drafted tokens over a cache (amk_tree_attention): q bf16 [n,
+    heads, head_dim]; k and v [rows, kv heads, head_dim] as in prompt_attention, with
+    at least pos + n rows; masks: n whole numbers, bit j of masks[i] set where token
+    i sees row pos + j (tree_masks gives a tree's)."""
+    a, out, device = _attention(q, k, v, scale, out)
+    n = q.shape[0]
+    if len(masks) != n:
+        raise ValueError(f"{len(masks)} masks for {n} tokens")
+    if n > AMK_TREE_MAX:
+        raise ValueError(f"a tree has at most {AMK_TREE_MAX} tokens, not {n}")
+    if pos < 0 or k.shape[0] < pos + n:
+        raise ValueError(f"k and v have {k.shape[0]} rows, tokens at {pos} need {pos + n}")
+    lib = load()
+    need = lib.amk_tree_attention_workspace(a.n_heads, a.n_kv_heads, a.head_dim, n, pos)
+    ws = _workspace(need, device)
+    _call(device, lib.amk_tree_attention, a, n, pos, (ctypes.c_uint64 * n)(*masks), ws.data_ptr() if need else None,
+          need, _stream(device))
+    return out
+
+
+def token_logprobs(logits, tokens=None, top: int = 0):
+    """(logprob, entropy, top_ids, top_logprobs) of rows of logits (amk_token_logprobs):
+    logits fp32, bf16 or fp16 [n, vocab] with contiguous rows; tokens int32 [n], or
+    None (logprob is then None); the `top` most probable tokens of each row."""
+    import torch
+    device = _cuda(logits, "logits")
+    types = {torch.float32: AMK_F32, torch.bfloat16: AMK_BF16, torch.float16: AMK_F16}
+    _tensor(logits, "logits", device, tuple(types), 2)
+    n, vocab = logits.shape
+    if n and vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have contiguous rows")
+    if not 0 <= top <= AMK_TOP_MAX:
+        raise ValueError(f"top must be in [0, {AMK_TOP_MAX}]")
+    logprob = None
+    if tokens is not None:
+        _tensor(tokens, "tokens", device, (torch.int32,), 1)
+        if not tokens.is_contiguous() or tokens.numel() != n:
+            raise ValueError(f"tokens must be {n} contiguous values")
+        logprob = torch.empty(n, dtype=torch.float32, device=device)
+    entropy = torch.empty(n, dtype=torch.float32, device=device)
+    ids = torch.empty(n, top, dtype=torch.int32, device=device)
+    values = torch.empty(n, top, dtype=torch.float32, device=device)
+    lib = load()
+    kind = types[logits.dtype]
+    need = lib.amk_token_logprobs_workspace(kind, n, vocab, top)
+    ws = _workspace(need, device)
+    _call(device, lib.amk_token_logprobs, logits.data_ptr(), kind, logits.stride(0) if n > 1 else vocab, n, vocab,
+          tokens.data_ptr() if logprob is not None else None, top, logprob.data_ptr() if logprob is not None else None,
+          entropy.data_ptr(), ids.data_ptr() if top else None, values.data_ptr() if top else None,
+          ws.data_ptr() if need else None, need, _stream(device))
+    return logprob, entropy, ids, values
+
+
+def kv_keep(kv, pos: int, rows) -> None:
+    """Move cache rows pos + rows[i] to pos + i in every layer and head (amk_kv_keep):
+    kv a contiguous 2-byte tensor [layers, 2, kv heads, max_seq, head_dim], rows
+    strictly ascending whole numbers."""
+    device = _cuda(kv, "kv")
+    if kv.dim() != 5 or kv.shape[1] != 2 or kv.element_size() != 2 or not kv.is_contiguous():
+        raise ValueError("kv must be a contiguous bf16 tensor [layers, 2, kv heads, max_seq, head_dim]")
+    layers, _, heads, cap, d = kv.shape
+    n = len(rows)
+    _call(device, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n,
+          _stream(device))
 
 
 # ---- convenience: a decoder over torch device tensors ---------------------------------
@@ -370,6 +621,60 @@ class Decoder:
             import torch
             stream = torch.cuda.current_stream().cuda_stream
         amk_decode_step(self.handle, token, pos, kv_cache.data_ptr(), logits.data_ptr(), stream)
+
+    def extend(self, tokens, pos: int, kv_cache, n_logits: Optional[int] = None, parents=None):
+        """Run several tokens through the model behind the `pos` positions in the cache
+        (amk_extend): a prompt or part of one, or, with `parents` (at most AMK_TREE_MAX
+        tokens, parents[i] in [-1, i)), a drafted tree.  Appends their K and V rows at
+        pos .. pos + n - 1 and returns the logits of the last n_logits tokens (default
+        all) as fp32 [n_logits, vocab], on torch's current stream."""
+        import torch
+        n = len(tokens)
+        n_logits = n if n_logits is None else n_logits
+        if not 0 <= n_logits <= n:
+            raise ValueError(f"n_logits must be in [0, {n}]")
+        if parents is not None and len(parents) != n:
+            raise ValueError(f"{len(parents)} parents for {n} tokens")
+        device = torch.device("cuda", self._dev)
+        need = amk_kv_cache_bytes(self.cfg)
+        if not kv_cache.is_cuda or kv_cache.device != device:
+            raise ValueError(f"kv_cache must be a tensor on {device}, the decoder's device")
+        if not kv_cache.is_contiguous() or kv_cache.numel() * kv_cache.element_size() < need:
+            raise ValueError(f"kv_cache must be contiguous with at least {need} bytes")
+        logits = torch.empty(n_logits, self.cfg.vocab, dtype=torch.float32, device=device)
+        if n == 0:
+            return logits
+        lib = load()
+        ws = _workspace(lib.amk_extend_workspace(self.handle, n), device)
+        ids = (ctypes.c_int32 * n)(*tokens)
+        par = None if parents is None else (ctypes.c_int32 * n)(*parents)
+        _call(device, lib.amk_extend, self.handle, ids, n, pos, par, kv_cache.data_ptr(),
+              logits.data_ptr() if n_logits else None, n_logits, ws.data_ptr(), ws.numel(), _stream(device))
+        return logits
+
+    def score(self, tokens, pos: int, kv_cache, top: int = 0):
+        """Score a text behind the `pos` positions in the cache: (logprob, entropy,
+        top_ids, top_logprobs) of tokens[1:], each given those before it
+        (token_logprobs over extend's logits).  Appends the rows of all its tokens."""
+        import torch
+        if len(tokens) < 2:
+            raise ValueError("a text to score has at least two tokens")
+        # the last token's logits predict what follows the text: not needed
+        logits = self.extend(tokens, pos, kv_cache)[:-1]
+        given = torch.tensor(list(tokens[1:]), dtype=torch.int32, device=logits.device)
+        return token_logprobs(logits, given, top)
+
+    def keep(self, pos: int, rows, kv_cache) -> None:
+        """After extend with a drafted tree at `pos`: make the accepted tokens' rows
+        (ascending indices into the tree) follow each other from pos on (amk_kv_keep)."""
+        c = self.cfg
+        shape = (c.n_layers, 2, c.n_kv_heads, c.max_seq, c.head_dim)
+        count = c.n_layers * 2 * c.n_kv_heads * c.max_seq * c.head_dim
+        if kv_cache.element_size() != 2 or not kv_cache.is_contiguous() or kv_cache.numel() < count:
+            raise ValueError(f"kv_cache must be contiguous 2-byte elements, at least {count}")
+        if not kv_cache.is_cuda or kv_cache.device.index != self._dev:
+            raise ValueError(f"kv_cache must be a tensor on cuda:{self._dev}, the decoder's device")
+        kv_keep(kv_cache.view(-1)[:count].view(shape), pos, rows)
 
     def next_token(self, stream: Optional[int] = None) -> int:
         if stream is None:

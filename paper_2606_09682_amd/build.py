@@ -24,7 +24,8 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", os.path.join(ROOT, "include"),
           "-Wall", "-Wno-unused-command-line-argument"]
 
-SOURCES = ["megakernel.hip", "schedule.cpp", "api.cpp"]
+SOURCES = ["megakernel.hip", "attention.hip", "linear.hip", "logprobs.hip", "extend.hip", "schedule.cpp", "api.cpp",
+           "ops_api.cpp"]
 # per-kernel register / scratch report of the device code, parsed from the
 # compiler's resource-usage remarks
 RESOURCES = os.path.join(BUILD, "resource_usage.txt")
@@ -37,19 +38,18 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def _compile(src: str) -> str:
+def _compile(src: str):
+    """Compile one source; returns (object path, resource report lines)."""
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
     extra = ["-Rpass-analysis=kernel-resource-usage"] if src.endswith(".hip") else []
     cmd = [hipcc()] + COMMON + DEVICE_FLAGS + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    if extra:
-        _write_resources(r.stderr)
-    return obj
+    return obj, _resources(r.stderr) if extra else []
 
 
-def _write_resources(remarks: str) -> None:
+def _resources(remarks: str) -> list:
     """One line per kernel: name, VGPRs, scratch bytes per lane, spilled VGPRs."""
     rows, cur = [], None
     for line in remarks.splitlines():
@@ -62,17 +62,19 @@ def _write_resources(remarks: str) -> None:
             rows.append(cur)
         elif cur is not None:
             cur[key] = val
-    with open(RESOURCES, "w") as f:
-        for r in rows:
-            f.write(f"{r['name']} vgprs={r.get('VGPRs')} scratch={r.get('ScratchSize [bytes/lane]')} "
-                    f"vgpr_spill={r.get('VGPRs Spill')}\n")
+    return [f"{r['name']} vgprs={r.get('VGPRs')} scratch={r.get('ScratchSize [bytes/lane]')} "
+            f"vgpr_spill={r.get('VGPRs Spill')}\n" for r in rows]
 
 
 def build(verbose: bool = False) -> str:
     """Compile every source and link libamk.so; returns its path."""
     os.makedirs(BUILD, exist_ok=True)
     with ThreadPoolExecutor(len(SOURCES)) as ex:
-        objs = list(ex.map(_compile, SOURCES))
+        done = list(ex.map(_compile, SOURCES))
+    objs = [obj for obj, _ in done]
+    with open(RESOURCES, "w") as f:
+        for _, lines in done:
+            f.writelines(lines)
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -13,6 +13,7 @@
 
 #include "../../include/amk.h"
 #include "device.h"
+#include "ops.h"
 #include "schedule.h"
 
 using amk::DevLayer;
@@ -52,6 +53,7 @@ struct amk_handle_s {
   DevSchedule dsch[kVariants];
   int last_variant = -1;
   DevModel dm;
+  std::vector<DevLayer> layers; // the layers' weight pointers, also in the device block
   void* d_block = nullptr;      // one device allocation for tables and scratch
   int32_t* h_status = nullptr;  // host-mapped
   int32_t* h_abort = nullptr;   // host-mapped
@@ -143,6 +145,34 @@ bool device_range(const void* p, size_t bytes, int device) {
   }
   const uintptr_t b = (uintptr_t)base, q = (uintptr_t)p;
   return q >= b && bytes <= size && q - b <= size - bytes;
+}
+
+// Most tokens amk_extend takes through the model at once: longer prompts go in
+// chunks, so its workspace stays bounded (the products are at their full rate
+// well before).
+constexpr int kExtendChunk = 2048;
+
+// amk_extend's workspace: byte offsets of its buffers for n tokens.
+struct ExtendLayout {
+  size_t x, h, qkv, q, o, gate, up, act, attn, bytes;
+};
+
+ExtendLayout extend_layout(const Shape& s, int n) {
+  const size_t c = (size_t)std::min(n, kExtendChunk), qd = (size_t)s.nq * s.hd, kd = (size_t)s.nkv * s.hd;
+  ExtendLayout r;
+  size_t top = 0;
+  auto take = [&](size_t bytes) { const size_t at = top; top = round_up(top + bytes, 256); return at; };
+  r.x = take(c * s.H * sizeof(float));
+  r.h = take(c * s.H * sizeof(uint16_t));
+  r.qkv = take(c * (qd + 2 * kd) * sizeof(float));
+  r.q = take(c * qd * sizeof(uint16_t));
+  r.o = take(c * qd * sizeof(uint16_t));
+  r.gate = take(c * s.I * sizeof(float));
+  r.up = take(c * s.I * sizeof(float));
+  r.act = take(c * s.I * sizeof(uint16_t));
+  r.attn = take(amk::attention_workspace_most(s.nq, s.nkv, s.hd));
+  r.bytes = top;
+  return r;
 }
 
 }  // namespace
@@ -492,6 +522,7 @@ static int create_impl(const amk_config_t* cfg, const amk_weights_t* w, const am
       layers[l].attn_norm = (const uint16_t*)lw.attn_norm;
       layers[l].mlp_norm = (const uint16_t*)lw.mlp_norm;
     }
+    h->layers = layers;
     // RoPE table: angle p * theta^(-2i/d), cos and sin evaluated in float64, stored float32
     std::vector<float> rope(2 * (size_t)s.max_seq * s.half);
     for (int i = 0; i < s.half; ++i) {
@@ -643,6 +674,115 @@ int amk_decode_step(amk_handle_t h, int32_t token, int32_t pos, void* kv_cache, 
   ds.epoch = epoch;
   h->last_stream = stream;
   h->launched = true;
+  return AMK_OK;
+}
+
+size_t amk_extend_workspace(amk_handle_t h, int32_t n) {
+  if (!h || n < 1) return 0;
+  return extend_layout(h->s, n).bytes;
+}
+
+int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, const int32_t* parents, void* kv_cache,
+               float* logits, int32_t n_logits, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || n < 0 || pos < 0 || n_logits < 0 || n_logits > n || (parents && n > AMK_TREE_MAX))
+    return AMK_ERR_INVALID_ARGUMENT;
+  const Shape& s = h->s;
+  if (n > s.max_seq - pos) return AMK_ERR_INVALID_ARGUMENT;
+  if (n == 0) return AMK_OK;
+  if (!tokens || !kv_cache || !workspace || (n_logits && !logits)) return AMK_ERR_INVALID_ARGUMENT;
+  if (((uintptr_t)kv_cache & 255u) != 0 || ((uintptr_t)workspace & 255u) != 0 || !aligned16(logits))
+    return AMK_ERR_INVALID_ARGUMENT;
+  for (int i = 0; i < n; ++i)
+    if (tokens[i] < 0 || tokens[i] >= s.V) return AMK_ERR_INVALID_ARGUMENT;
+  amk::TreeDepths depths = {};
+  amk::TreeMasks masks = {};
+  for (int i = 0; i < n && n <= AMK_TREE_MAX; ++i) {
+    const int parent = parents ? parents[i] : i - 1;
+    if (parent < -1 || parent >= i) return AMK_ERR_INVALID_ARGUMENT;
+    depths.at[i] = parent < 0 ? 0 : depths.at[parent] + 1;
+    masks.bits[i] = 1ull << i | (parent < 0 ? 0 : masks.bits[parent]);
+  }
+  DeviceGuard guard(h->device);
+  if (!guard.ok) return AMK_ERR_DEVICE;
+  const ExtendLayout lay = extend_layout(s, n);
+  if (workspace_bytes < lay.bytes || !device_range(workspace, lay.bytes, h->device) ||
+      !device_range(kv_cache, amk_kv_cache_bytes_of(s), h->device) ||
+      (n_logits && !device_range(logits, sizeof(float) * (size_t)s.V * n_logits, h->device)))
+    return AMK_ERR_INVALID_ARGUMENT;
+
+  char* base = (char*)workspace;
+  float* x = (float*)(base + lay.x);
+  uint16_t* hb = (uint16_t*)(base + lay.h);
+  float* qkv = (float*)(base + lay.qkv);
+  uint16_t* q = (uint16_t*)(base + lay.q);
+  uint16_t* o = (uint16_t*)(base + lay.o);
+  float* gate = (float*)(base + lay.gate);
+  float* up = (float*)(base + lay.up);
+  uint16_t* act = (uint16_t*)(base + lay.act);
+  void* attn_ws = base + lay.attn;
+  const int H = s.H, I = s.I, qd = s.nq * s.hd, kd = s.nkv * s.hd, qkvd = qd + 2 * kd;
+  const int64_t plane = (int64_t)s.max_seq * s.hd;
+
+  auto linear = [&](const uint16_t* in, int width, int rows, const void* w, const void* sc, int fmt, int out, float* y,
+                    int64_t y_stride, int accumulate) {
+    amk::LinearArgs a;
+    a.x = in; a.x_stride = width; a.n = rows; a.in = width; a.out = out; a.w = w; a.scale = sc; a.fmt = fmt;
+    a.group = s.qgroup; a.y = y; a.y_stride = y_stride; a.y_bf16 = 0; a.accumulate = accumulate;
+    return amk::launch_linear(a, stream);
+  };
+
+  // long prompts go through the model in chunks, each behind the one before
+  for (int c0 = 0; c0 < n; c0 += kExtendChunk) {
+    const int c = std::min(kExtendChunk, n - c0), at = pos + c0;
+    int st = AMK_OK;
+    for (int t0 = 0; t0 < c && st == AMK_OK; t0 += amk::kTokensPerLaunch) {
+      amk::TokenBlock ids = {};
+      const int m = std::min(amk::kTokensPerLaunch, c - t0);
+      std::memcpy(ids.id, tokens + c0 + t0, sizeof(int32_t) * (size_t)m);
+      st = amk::launch_embed(h->dm.embed, ids, m, H, x + (size_t)t0 * H, stream);
+    }
+    if (c <= AMK_TREE_MAX && n > AMK_TREE_MAX)  // the last chunk of a prompt: a chain of its own
+      for (int i = 0; i < c; ++i) {
+        depths.at[i] = i;
+        masks.bits[i] = i == 63 ? ~0ull : (2ull << i) - 1;
+      }
+    for (int l = 0; l < s.L && st == AMK_OK; ++l) {
+      const DevLayer& w = h->layers[l];
+      uint16_t* k = (uint16_t*)kv_cache + (int64_t)l * 2 * s.nkv * plane;
+      uint16_t* v = k + s.nkv * plane;
+      if (st == AMK_OK) st = amk::launch_rmsnorm(x, w.attn_norm, c, H, s.eps, hb, stream);
+      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_Q], w.s[amk::W_Q], s.fmt, qd, qkv, qkvd, 0);
+      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_K], w.s[amk::W_K], s.fmt, kd, qkv + qd, qkvd, 0);
+      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_V], w.s[amk::W_V], s.fmt, kd, qkv + qd + kd, qkvd, 0);
+      if (st == AMK_OK)
+        st = amk::launch_rope_append(qkv, h->dm.rope, c, at, parents ? &depths : nullptr, s.nq, s.nkv, s.hd, s.max_seq,
+                                     q, k, v, stream);
+      amk_attention_t a = {q, k, v, o, qd, s.hd, s.hd, plane, s.hd, plane, qd, s.hd, s.nq, s.nkv, s.hd,
+                           h->dm.attn_scale};
+      if (st == AMK_OK) {
+        if (c <= AMK_TREE_MAX)
+          st = amk::launch_tree(a, amk::tree_plan(s.nq, s.nkv, s.hd, c, at), c, at, masks, attn_ws, stream);
+        else
+          st = amk::launch_prompt(a, amk::prompt_plan(s.nq, s.nkv, s.hd, 1, c, at + c), nullptr, nullptr, 1, c, at + c,
+                                  attn_ws, stream);
+      }
+      if (st == AMK_OK) st = linear(o, qd, c, w.w[amk::W_O], w.s[amk::W_O], s.fmt, H, x, H, 1);
+      if (st == AMK_OK) st = amk::launch_rmsnorm(x, w.mlp_norm, c, H, s.eps, hb, stream);
+      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_G], w.s[amk::W_G], s.fmt, I, gate, I, 0);
+      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_U], w.s[amk::W_U], s.fmt, I, up, I, 0);
+      if (st == AMK_OK) st = amk::launch_silu_mul(gate, up, (int64_t)c * I, act, stream);
+      if (st == AMK_OK) st = linear(act, I, c, w.w[amk::W_D], w.s[amk::W_D], s.fmt, H, x, H, 1);
+    }
+    // logits of this chunk's tokens among the last n_logits
+    const int first = std::max(c0, n - n_logits), m = c0 + c - first;
+    if (st == AMK_OK && m > 0) {
+      st = amk::launch_rmsnorm(x + (size_t)(first - c0) * H, h->dm.final_norm, m, H, s.eps, hb, stream);
+      if (st == AMK_OK)
+        st = linear(hb, H, m, h->dm.lm_w, h->dm.lm_s, h->dm.lm_fmt, s.V, logits + (int64_t)(first - (n - n_logits)) * s.V,
+                    s.V, 0);
+    }
+    if (st != AMK_OK) return st;
+  }
   return AMK_OK;
 }
 

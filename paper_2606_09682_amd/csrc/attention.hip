@@ -1,0 +1,457 @@
+// Attention of several tokens: whole prompts (causal, packed sequences) and
+// drafted trees over a KV cache.
+//
+// O = softmax(Q K^T scale) V per query head, in one pass over the keys with the
+// running maximum m and sum l of each row: a tile of keys gives scores s, m' =
+// max(m, max s), p = 2^(s - m') (scores in units of log2), l = l 2^(m - m') +
+// sum p, O = O 2^(m - m') + p V, and O / l at the end.
+//
+// Rows.  The query heads of a KV group read the same K and V, so a workgroup's
+// rows are (token, head of the group) pairs, row = token * group + head: K and V
+// are staged once for all of them, and a causal tile of 128 rows spans few
+// tokens, which leaves little masked work at the diagonal.
+//
+// Matrix cores.  Scores are taken transposed, S^T = K Q^T (32x32x16 bf16 tiles):
+// a lane then holds keys of one query row, so the row's maximum and sum are
+// taken within the lane and across one other lane.  The registers of S^T, rounded
+// to bf16, are the B operand of O^T = V^T P^T as they lie, if the product's k slots
+// 0..7 of lane half h stand for keys 4h..4h+3 and 8+4h..8+4h+3 of each 16: V^T's
+// operand is read from the row-major tile in exactly that order by the
+// transposed LDS reads.  P is rounded to bf16 (relative error at most 2^-8, of
+// the size of the output's own rounding); l sums the unrounded p in fp32.
+//
+// LDS.  K and V tiles are loaded straight to LDS (16 bytes a lane), two stages,
+// so a tile's loads run under the previous tile's products.  Rows lie without
+// padding, their 16-byte chunks permuted by the row so that neither the K reads
+// (32 rows at one column) nor the transposed V reads (4 rows x 32 bytes) meet in
+// a bank.
+//
+// Masked keys.  A score outside a row's keys is replaced, not added to.  p is
+// then 0, but 0 * V is NaN where V holds an infinity or NaN, so tiles that some
+// row sees only in part are looked through for such values; if there are any,
+// the tile's product is taken key by key over visible keys alone.
+#include <algorithm>
+#include <cmath>
+
+#include "ops.h"
+#include "ops_device.h"
+
+namespace amk {
+namespace {
+
+struct AttnArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  int32_t n_heads, n_kv, group;
+  float scale2;       // scale * log2(e)
+  int32_t splits, tiles;
+  int32_t total_q, total_k;
+  float* part_o;      // [splits][total_q * n_heads][head_dim], unnormalised
+  float2* part_ml;    // [splits][total_q * n_heads] (m, l)
+};
+
+struct PromptArgs {
+  const int32_t *cu_q, *cu_k;  // null: one sequence
+  int32_t n_seqs;
+};
+
+struct TreeArgs {
+  int32_t pos;
+  TreeMasks masks;
+};
+
+// What one workgroup works on.
+struct Span {
+  int32_t q0, nq;     // queries of the sequence
+  int32_t k0, nk;     // its keys
+  int32_t tile;       // row tile within it; negative: none
+};
+
+__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Row tile `tile` counted over all sequences: each wave looks at 64 sequences at
+// a time and adds up their tiles.
+__device__ Span find_span(const AttnArgs& a, const PromptArgs& p, int tile, int rows_per_tile) {
+  if (!p.cu_q) return {0, a.total_q, 0, a.total_k, tile};
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < p.n_seqs; base += 64) {
+    const int b = base + lane;
+    Span s = {0, 0, 0, 0, -1};
+    int mine = 0;
+    if (b < p.n_seqs) {
+      s.q0 = clamp_to(p.cu_q[b], 0, a.total_q);
+      s.nq = clamp_to(p.cu_q[b + 1], s.q0, a.total_q) - s.q0;
+      s.k0 = clamp_to(p.cu_k[b], 0, a.total_k);
+      s.nk = clamp_to(p.cu_k[b + 1], s.k0, a.total_k) - s.k0;
+      mine = (int)(((int64_t)s.nq * a.group + rows_per_tile - 1) / rows_per_tile);
+    }
+    int upto = mine;  // inclusive sum over the lanes
+    for (int d = 1; d < 64; d <<= 1) {
+      const int t = __shfl_up(upto, d);
+      if (lane >= d) upto += t;
+    }
+    const uint64_t past = __ballot(tile < upto);
+    if (past) {
+      const int src = __ffsll((unsigned long long)past) - 1;
+      s.tile = tile - (upto - mine);
+      return {__shfl(s.q0, src), __shfl(s.nq, src), __shfl(s.k0, src), __shfl(s.nk, src), __shfl(s.tile, src)};
+    }
+    tile -= __shfl(upto, 63);
+  }
+  return {0, 0, 0, 0, -1};
+}
+
+__device__ __forceinline__ Span find_span(const AttnArgs& a, const TreeArgs& t, int tile, int) {
+  return {0, a.total_q, 0, a.total_k, tile};
+}
+
+// The keys a row sees: all below `full`, and key full + j where bit j of `bits` is set.
+struct Sees {
+  int32_t full;
+  uint64_t bits;
+  __device__ __forceinline__ bool at(int key) const {
+    const int j = key - full;
+    return j < 0 || (j < 64 && (bits >> j & 1));
+  }
+};
+
+__device__ __forceinline__ Sees sees_of(const PromptArgs&, const Span& s, int token) {
+  return {max(0, s.nk - s.nq + token + 1), 0};
+}
+__device__ __forceinline__ Sees sees_of(const TreeArgs& t, const Span&, int token) {
+  return {t.pos, t.masks.bits[token]};
+}
+
+// Keys the tokens up to `token` may see at all.
+__device__ __forceinline__ int last_key(const PromptArgs&, const Span& s, int token) {
+  return clamp_to(s.nk - s.nq + token + 1, 0, s.nk);
+}
+__device__ __forceinline__ int last_key(const TreeArgs&, const Span& s, int) { return s.nk; }
+
+template <int HD>
+__device__ __forceinline__ int k_swizzle(int row) {
+  return HD == 128 ? row & 15 : (row >> 1) & 7;
+}
+template <int HD>
+__device__ __forceinline__ int v_swizzle(int row) {
+  return HD == 128 ? (row & 3) << 2 : (row & 2) << 1;
+}
+
+template <int HD, int WAVES, int BN, typename Which>
+__global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, const Which w) {
+  constexpr int ROWS = 32 * WAVES, CPR = HD / 8, KB = BN / 32, DB = HD / 32;
+  constexpr int TILE = BN * HD;                      // elements of a K or V tile
+  constexpr int LOADS = TILE / 8 / (64 * WAVES);     // 16-byte loads per lane and tile
+  static_assert(LOADS >= 1 && TILE % (8 * 64 * WAVES) == 0, "whole loads");
+  constexpr int WEIGHTS = WAVES * 32 * BN;           // p of all waves, where products are taken key by key
+  __shared__ __align__(16) uint16_t lds[2][2][TILE];  // [stage][K, V]
+  __shared__ __align__(16) uint16_t more[WEIGHTS > TILE ? WEIGHTS : 8];
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int half = lane >> 5, col = lane & 31;
+  const int kvh = blockIdx.x % a.n_kv;
+  const int rest = blockIdx.x / a.n_kv;
+  const int split = rest % a.splits;
+  // later tiles of a causal prompt have more keys: the last ones start first
+  const Span s = find_span(a, w, a.tiles - 1 - rest / a.splits, ROWS);
+  if (s.tile < 0) return;
+  const int rows = s.nq * a.group, row0 = s.tile * ROWS;
+  if (row0 >= rows) return;
+  const int last_row = min(rows, row0 + ROWS) - 1;
+
+  const int row = row0 + wave * 32 + col;
+  const bool valid = row <= last_row;
+  const int token = valid ? row / a.group : 0, head = valid ? kvh * a.group + row % a.group : 0;
+  Sees sees = {0, 0};
+  if (valid) sees = sees_of(w, s, token);
+  const int kend = last_key(w, s, last_row / a.group);
+  const int kfull = min(sees_of(w, s, row0 / a.group).full, kend);  // seen by every row of the tile
+
+  bf16x8 q[HD / 16];
+  {
+    const uint16_t* qp = a.q + (s.q0 + token) * a.q_token + head * a.q_head + half * 8;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) {
+      u32x4 v = {0, 0, 0, 0};
+      if (valid) v = *(const u32x4*)(qp + 16 * i);
+      q[i] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+
+  const int ktiles = (kend + BN - 1) / BN;
+  const int t0 = (int)((int64_t)ktiles * split / a.splits), t1 = (int)((int64_t)ktiles * (split + 1) / a.splits);
+  const uint16_t* kp = a.k + s.k0 * a.k_token + kvh * a.k_head;
+  const uint16_t* vp = a.v + s.k0 * a.v_token + kvh * a.v_head;
+
+  // rows past the last key repeat it: in range, and masked
+  auto load_tile = [&](int t, int stage) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int c0 = (i * WAVES + wave) * 64, c = c0 + lane;
+      const int r = c / CPR, at = c % CPR;
+      const int64_t key = min(t * BN + r, s.nk - 1);
+      load_lds16(kp + key * a.k_token + (at ^ k_swizzle<HD>(r)) * 8, &lds[stage][0][c0 * 8]);
+      load_lds16(vp + key * a.v_token + (at ^ v_swizzle<HD>(r)) * 8, &lds[stage][1][c0 * 8]);
+    }
+  };
+
+  f32x16 o[DB] = {};
+  float m = -INFINITY, l = 0.f;
+  if (t0 < t1) load_tile(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int stage = (t - t0) & 1;
+    wait_loads();
+    __syncthreads();  // this tile's loads are in, the other stage's readers are done
+    if (t + 1 < t1) load_tile(t + 1, stage ^ 1);
+    const uint16_t* kt = lds[stage][0];
+    const uint16_t* vt = lds[stage][1];
+
+    f32x16 sc[KB] = {};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        const int r = kb * 32 + col;
+        const bf16x8 kf = *(const bf16x8*)(kt + r * HD + ((2 * i + half) ^ k_swizzle<HD>(r)) * 8);
+        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
+      }
+
+    const bool partial = t * BN + BN > kfull;  // the same for the whole workgroup
+    if (partial) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = t * BN + kb * 32 + 8 * (i / 4) + 4 * half + i % 4;
+          if (key >= kend || !sees.at(key)) sc[kb][i] = -INFINITY;
+        }
+    }
+
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m_new = fmaxf(m, top * a.scale2);
+    const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: p = 2^-inf = 0
+    const float keep = __builtin_amdgcn_exp2f(m - base);
+    m = m_new;
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], a.scale2, -base));
+        sum += sc[kb][i];
+      }
+    l = l * keep + sum;
+    if (__any(keep != 1.f)) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+    }
+
+    bf16x8 p[KB][2];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[kb][i / 8][i % 8] = (__bf16)sc[kb][i];
+
+    bool odd = false;
+    if (partial) {
+      for (int c = threadIdx.x; c < TILE / 8; c += 64 * WAVES) {
+        const u32x4 x = *(const u32x4*)(vt + c * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+      }
+      odd = __syncthreads_or(odd);
+    }
+    if (!odd) {
+      const int vr = 4 * half + (lane & 15) / 4;  // + multiples of 8
+      const int vc = ((lane >> 4) & 1) * 2 + (lane & 3) / 2, ve = (lane & 1) * 4;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const uint16_t* at = vt + (kb * 32 + ks * 16 + vr) * HD + ((4 * d + vc) ^ v_swizzle<HD>(vr)) * 8 + ve;
+            const s16x4 lo = read_tr16(at), hi = read_tr16(at + 8 * HD);
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), p[kb][ks], o[d], 0, 0, 0);
+          }
+    } else {
+      // key by key: the weights go through the K tile, which every wave has read, if they fit
+      uint16_t* pt = (WEIGHTS > TILE ? more : lds[stage][0]) + (wave * 32 + col) * BN;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pt[kb * 32 + 8 * (i / 4) + 4 * half + i % 4] = f32_to_bf16(sc[kb][i]);
+      __syncthreads();
+      for (int j = 0; j < BN; ++j) {
+        const int key = t * BN + j;
+        if (key >= kend || !sees.at(key)) continue;
+        const float pj = bf16_to_f32(pt[j]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+            o[d][i] += pj * bf16_to_f32(vt[j * HD + ((e / 8) ^ v_swizzle<HD>(j)) * 8 + e % 8]);
+          }
+      }
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  if (!valid) return;
+  if (a.splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* op = a.out + (s.q0 + token) * a.out_token + head * a.out_head + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x2 v = {pack_bf16(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                         pack_bf16(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
+        *(u32x2*)(op + 32 * d + 8 * i) = v;
+      }
+  } else {
+    const int64_t at = ((int64_t)split * a.total_q + s.q0 + token) * a.n_heads + head;
+    if (half == 0) a.part_ml[at] = make_float2(m, l);
+    float* op = a.part_o + at * HD + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 v = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        *(f32x4*)(op + 32 * d + 8 * i) = v;
+      }
+  }
+}
+
+// Joins the splits of each (token, head): one wave each, HD / 64 elements a lane.
+// Splits that saw nothing for the row (l = 0) are left out.
+template <int HD>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, const int32_t* cu_q, int32_t n_seqs) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.total_q * a.n_heads;
+  if (at >= all) return;
+  const int64_t token = at / a.n_heads;
+  const int head = (int)(at % a.n_heads);
+  if (cu_q && (token < cu_q[0] || token >= cu_q[n_seqs])) return;
+  float m = -INFINITY;
+  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, a.part_ml[i * all + at].x);
+  const float base = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[HD / 64] = {};
+  for (int i = 0; i < a.splits; ++i) {
+    const float2 ml = a.part_ml[i * all + at];
+    if (ml.y == 0.f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml.x - base);
+    l += f * ml.y;
+#pragma unroll
+    for (int e = 0; e < HD / 64; ++e) o[e] += f * a.part_o[(i * all + at) * HD + lane * (HD / 64) + e];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* op = a.out + token * a.out_token + head * a.out_head + lane * (HD / 64);
+#pragma unroll
+  for (int e = 0; e < HD / 64; ++e) op[e] = f32_to_bf16(o[e] * inv);
+}
+
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+AttnPlan with_workspace(AttnPlan p, int n_heads, int head_dim, int total_q) {
+  const size_t rows = (size_t)p.splits * total_q * n_heads;
+  p.workspace = p.splits == 1 ? 0 : up256(rows * head_dim * sizeof(float)) + rows * sizeof(float2);
+  return p;
+}
+
+constexpr int kSplitBlocks = 1024;  // workgroups that splits of the keys may add up to
+
+int waves_for(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+AttnArgs make_args(const amk_attention_t& a, const AttnPlan& p, int total_q, int total_k, void* workspace) {
+  AttnArgs r;
+  r.q = (const uint16_t*)a.q; r.k = (const uint16_t*)a.k; r.v = (const uint16_t*)a.v; r.out = (uint16_t*)a.out;
+  r.q_token = a.q_token; r.q_head = a.q_head; r.k_token = a.k_token; r.k_head = a.k_head;
+  r.v_token = a.v_token; r.v_head = a.v_head; r.out_token = a.out_token; r.out_head = a.out_head;
+  r.n_heads = a.n_heads; r.n_kv = a.n_kv_heads; r.group = a.n_heads / a.n_kv_heads;
+  r.scale2 = (float)((double)a.scale * 1.4426950408889634);
+  r.splits = p.splits; r.tiles = p.tiles; r.total_q = total_q; r.total_k = total_k;
+  r.part_o = (float*)workspace;
+  r.part_ml = (float2*)((char*)workspace + up256((size_t)p.splits * total_q * a.n_heads * a.head_dim * sizeof(float)));
+  return r;
+}
+
+template <int HD, typename Which>
+void launch_hd(const AttnArgs& r, const AttnPlan& p, const Which& w, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)p.tiles * p.splits * r.n_kv));
+  if (p.waves == 1) hipLaunchKernelGGL((attn_kernel<HD, 1, 32, Which>), grid, dim3(64), 0, st, r, w);
+  else if (p.waves == 2) hipLaunchKernelGGL((attn_kernel<HD, 2, 32, Which>), grid, dim3(128), 0, st, r, w);
+  else hipLaunchKernelGGL((attn_kernel<HD, 4, 64, Which>), grid, dim3(256), 0, st, r, w);
+}
+
+template <typename Which>
+int launch_attn(const AttnArgs& r, const AttnPlan& p, int head_dim, const Which& w, const int32_t* cu_q, int n_seqs,
+                hipStream_t st) {
+  if (head_dim == 128) launch_hd<128>(r, p, w, st);
+  else launch_hd<64>(r, p, w, st);
+  if (hipGetLastError() != hipSuccess) return AMK_ERR_DEVICE;
+  if (p.splits > 1) {
+    const dim3 grid((unsigned)(((int64_t)r.total_q * r.n_heads + 3) / 4));
+    if (head_dim == 128) hipLaunchKernelGGL(attn_join_kernel<128>, grid, dim3(256), 0, st, r, cu_q, n_seqs);
+    else hipLaunchKernelGGL(attn_join_kernel<64>, grid, dim3(256), 0, st, r, cu_q, n_seqs);
+    if (hipGetLastError() != hipSuccess) return AMK_ERR_DEVICE;
+  }
+  return AMK_OK;
+}
+
+}  // namespace
+
+AttnPlan prompt_plan(int n_heads, int n_kv_heads, int head_dim, int n_seqs, int total_q, int total_k) {
+  AttnPlan p;
+  const int64_t rows = (int64_t)total_q * (n_heads / n_kv_heads);
+  p.waves = waves_for(rows);
+  // whole tiles of the sum, and one that is not whole per sequence
+  p.tiles = (int)(rows / (32 * p.waves) + std::min<int64_t>(n_seqs, rows));
+  const int64_t blocks = (int64_t)p.tiles * n_kv_heads;
+  // few row tiles leave CUs without work: split their keys, in ranges of 256 at least
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitBlocks / 2 / blocks, ((int64_t)total_k + 255) / 256));
+  return with_workspace(p, n_heads, head_dim, total_q);
+}
+
+AttnPlan tree_plan(int n_heads, int n_kv_heads, int head_dim, int n, int pos) {
+  AttnPlan p;
+  const int64_t rows = (int64_t)n * (n_heads / n_kv_heads);
+  p.waves = waves_for(rows);
+  p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+  const int64_t blocks = (int64_t)p.tiles * n_kv_heads;
+  // about kSplitBlocks workgroups, of 128 keys at least
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitBlocks / blocks, ((int64_t)pos + n + 127) / 128));
+  return with_workspace(p, n_heads, head_dim, n);
+}
+
+size_t attention_workspace_most(int n_heads, int n_kv_heads, int head_dim) {
+  // a plan with splits has at most kSplitBlocks workgroups of at most 128 rows
+  const size_t rows = (size_t)kSplitBlocks * 128;
+  return up256(rows * head_dim * sizeof(float)) + rows * sizeof(float2);
+}
+
+int launch_prompt(const amk_attention_t& a, const AttnPlan& p, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,
+                  int total_q, int total_k, void* workspace, void* stream) {
+  return launch_attn(make_args(a, p, total_q, total_k, workspace), p, a.head_dim, PromptArgs{cu_q, cu_k, n_seqs}, cu_q,
+                     n_seqs, (hipStream_t)stream);
+}
+
+int launch_tree(const amk_attention_t& a, const AttnPlan& p, int n, int pos, const TreeMasks& m, void* workspace,
+                void* stream) {
+  return launch_attn(make_args(a, p, n, pos + n, workspace), p, a.head_dim, TreeArgs{pos, m}, nullptr, 0,
+                     (hipStream_t)stream);
+}
+
+}  // namespace amk
