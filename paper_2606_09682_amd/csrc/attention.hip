@@ -32,6 +32,7 @@
 // the tile's product is taken key by key over visible keys alone.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -110,9 +111,13 @@ __device__ __forceinline__ Span find_span(const AttnArgs& a, const TreeArgs& t, 
 struct Sees {
   int32_t full;
   uint64_t bits;
-  __device__ __forceinline__ bool at(int key) const {
-    const int j = key - full;
-    return j < 0 || (j < 64 && (bits >> j & 1));
+  // bit i: whether it sees key + i (0 <= i < 32), as far as key + i < end
+  __device__ __forceinline__ uint32_t word(int key, int end) const {
+    const int past = key - full;  // the first bit's place in `bits`
+    uint64_t w = past <= -32 ? ~0ull : past < 0 ? bits << -past | ((1ull << -past) - 1) : past < 64 ? bits >> past : 0;
+    const int room = end - key;
+    if (room < 32) w &= room > 0 ? (1ull << room) - 1 : 0;
+    return (uint32_t)w;
   }
 };
 
@@ -139,7 +144,7 @@ __device__ __forceinline__ int v_swizzle(int row) {
 }
 
 template <int HD, int WAVES, int BN, typename Which>
-__global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, const Which w) {
+__global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, const Which w) {
   constexpr int ROWS = 32 * WAVES, CPR = HD / 8, KB = BN / 32, DB = HD / 32;
   constexpr int TILE = BN * HD;                      // elements of a K or V tile
   constexpr int LOADS = TILE / 8 / (64 * WAVES);     // 16-byte loads per lane and tile
@@ -183,23 +188,40 @@ __global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, cons
   const int t0 = (int)((int64_t)ktiles * split / a.splits), t1 = (int)((int64_t)ktiles * (split + 1) / a.splits);
   const uint16_t* kp = a.k + s.k0 * a.k_token + kvh * a.k_head;
   const uint16_t* vp = a.v + s.k0 * a.v_token + kvh * a.v_head;
+  // this lane's chunk of a tile's first rows; later rows of a load follow STEP apart
+  constexpr int STEP = 64 * WAVES / CPR;
+  const int lr = threadIdx.x / CPR, lc = threadIdx.x % CPR;
+  const int vc0 = (lc ^ v_swizzle<HD>(lr)) * 8;
+  static_assert(STEP % 4 == 0, "V rows of a lane share their permutation");
 
-  // rows past the last key repeat it: in range, and masked
   auto load_tile = [&](int t, int stage) {
+    uint16_t* to = &lds[stage][0][wave * 512];
+    if (t * BN + BN <= s.nk) {
+      const uint16_t* kl = kp + (int64_t)(t * BN) * a.k_token + lr * a.k_token;
+      const uint16_t* vl = vp + (int64_t)(t * BN) * a.v_token + lr * a.v_token + vc0;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int c0 = (i * WAVES + wave) * 64, c = c0 + lane;
-      const int r = c / CPR, at = c % CPR;
-      const int64_t key = min(t * BN + r, s.nk - 1);
-      load_lds16(kp + key * a.k_token + (at ^ k_swizzle<HD>(r)) * 8, &lds[stage][0][c0 * 8]);
-      load_lds16(vp + key * a.v_token + (at ^ v_swizzle<HD>(r)) * 8, &lds[stage][1][c0 * 8]);
+      for (int i = 0; i < LOADS; ++i) {
+        const int kc = (lc ^ k_swizzle<HD>(lr + i * STEP)) * 8;
+        load_lds16(kl + i * STEP * a.k_token + kc, to + i * WAVES * 512);
+        load_lds16(vl + i * STEP * a.v_token, to + i * WAVES * 512 + TILE);
+      }
+    } else {  // rows past the last key repeat it: in range, and masked
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int kc = (lc ^ k_swizzle<HD>(lr + i * STEP)) * 8;
+        const int64_t key = min(t * BN + i * STEP + lr, s.nk - 1);
+        load_lds16(kp + key * a.k_token + kc, to + i * WAVES * 512);
+        load_lds16(vp + key * a.v_token + vc0, to + i * WAVES * 512 + TILE);
+      }
     }
   };
 
   f32x16 o[DB] = {};
   float m = -INFINITY, l = 0.f;
-  if (t0 < t1) load_tile(t0, 0);
-  for (int t = t0; t < t1; ++t) {
+
+  // one tile of keys; PARTIAL: some row sees only some of them
+  auto step = [&](const int t, auto partial) {
+    constexpr bool PARTIAL = decltype(partial)::value;
     const int stage = (t - t0) & 1;
     wait_loads();
     __syncthreads();  // this tile's loads are in, the other stage's readers are done
@@ -217,15 +239,14 @@ __global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, cons
         sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
       }
 
-    const bool partial = t * BN + BN > kfull;  // the same for the whole workgroup
-    if (partial) {
+    if constexpr (PARTIAL) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < KB; ++kb) {
+        const uint32_t word = sees.word(t * BN + kb * 32, kend) >> 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = t * BN + kb * 32 + 8 * (i / 4) + 4 * half + i % 4;
-          if (key >= kend || !sees.at(key)) sc[kb][i] = -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i)
+          if (!(word >> (8 * (i / 4) + i % 4) & 1)) sc[kb][i] = -INFINITY;
+      }
     }
 
     float top = -INFINITY;
@@ -261,7 +282,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, cons
       for (int i = 0; i < 16; ++i) p[kb][i / 8][i % 8] = (__bf16)sc[kb][i];
 
     bool odd = false;
-    if (partial) {
+    if constexpr (PARTIAL) {
       for (int c = threadIdx.x; c < TILE / 8; c += 64 * WAVES) {
         const u32x4 x = *(const u32x4*)(vt + c * 8);
 #pragma unroll
@@ -294,8 +315,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, cons
         for (int i = 0; i < 16; ++i) pt[kb * 32 + 8 * (i / 4) + 4 * half + i % 4] = f32_to_bf16(sc[kb][i]);
       __syncthreads();
       for (int j = 0; j < BN; ++j) {
-        const int key = t * BN + j;
-        if (key >= kend || !sees.at(key)) continue;
+        if (!(sees.word(t * BN + j, kend) & 1)) continue;
         const float pj = bf16_to_f32(pt[j]);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -306,7 +326,11 @@ __global__ void __launch_bounds__(64 * WAVES) attn_kernel(const AttnArgs a, cons
           }
       }
     }
-  }
+  };
+  const int tf = max(t0, min(t1, kfull / BN));  // tiles that every row sees whole
+  if (t0 < t1) load_tile(t0, 0);
+  for (int t = t0; t < tf; ++t) step(t, std::false_type());
+  for (int t = tf; t < t1; ++t) step(t, std::true_type());
 
   l += __shfl_xor(l, 32);
   if (!valid) return;
