@@ -27,12 +27,11 @@
 // a bank.
 //
 // Masked keys.  A score outside a row's keys is replaced, not added to.  p is
-// then 0, but 0 * V is NaN where V holds an infinity or NaN, so tiles that some
-// row sees only in part are looked through for such values; if there are any,
-// the tile's product is taken key by key over visible keys alone.
+// then 0, but 0 * V is NaN where V holds an infinity or NaN, so in tiles that
+// some row sees only in part such values of V are set to 0 before the product;
+// if there were any, they are added at the end to the rows that see their key.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -143,15 +142,168 @@ __device__ __forceinline__ int v_swizzle(int row) {
   return HD == 128 ? (row & 3) << 2 : (row & 2) << 1;
 }
 
+// Where a workgroup's tiles of K and V come from: this lane's chunk of their first rows.
+template <int HD, int WAVES, int BN>
+struct Source {
+  static constexpr int CPR = HD / 8;                    // 16-byte chunks per row
+  static constexpr int LOADS = BN * CPR / (64 * WAVES); // loads per lane and tile
+  static constexpr int STEP = 64 * WAVES / CPR;         // rows from one load of a lane to its next
+  static_assert(LOADS >= 1 && STEP % 4 == 0, "whole loads, whose V rows share their permutation");
+  const uint16_t *k, *v;  // the KV head's rows
+  int64_t k_token, v_token;
+  int32_t nk;
+
+  // This lane's chunks of tile t: where they are in K and V.
+  __device__ __forceinline__ void chunks(int t, const uint16_t* (&kc)[LOADS], const uint16_t* (&vc)[LOADS]) const {
+    const int row = threadIdx.x / CPR, chunk = threadIdx.x % CPR;
+    const uint16_t *kt = k + (int64_t)(t * BN) * k_token, *vt = v + (int64_t)(t * BN) * v_token;
+    const int left = nk - 1 - t * BN;  // rows past the last key repeat it: in range, and masked
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int64_t r = min(i * STEP + row, left);
+      kc[i] = kt + r * k_token + (chunk ^ k_swizzle<HD>(row + i * STEP)) * 8;
+      vc[i] = vt + r * v_token + (chunk ^ v_swizzle<HD>(row)) * 8;
+    }
+  }
+
+  __device__ __forceinline__ void tile(int t, AMK_LDS uint16_t* to) const {
+    const uint16_t *kc[LOADS], *vc[LOADS];
+    chunks(t, kc, vc);
+    to += threadIdx.x / 64 * 512;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      load_lds16(kc[i], to + i * WAVES * 512);
+      load_lds16(vc[i], to + i * WAVES * 512 + BN * HD);
+    }
+  }
+};
+
+// The running result of this lane's query row: half of the columns of O, and m and l
+// (l of the lane's own keys only).
+template <int HD>
+struct Running {
+  f32x16 o[HD / 32];
+  float m, l;
+  int odd;  // values of V were set to 0
+};
+
+// Takes tile t, which lies in kt and vt, into the running result, while tile t + 1 (if
+// more follow) is loaded into `next`.  PARTIAL: some row sees only some of the keys.
+// kt, vt, next and odd do not overlap: without that promise, which the compiler follows for
+// pointers of few uses only, every read of tile t would wait for the loads of tile t + 1.
+template <int HD, int WAVES, int BN, bool PARTIAL>
+__device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int t, bool more,
+                                          const AMK_LDS uint16_t* __restrict__ kt,
+                                          AMK_LDS uint16_t* __restrict__ vt, AMK_LDS uint16_t* __restrict__ next,
+                                          AMK_LDS int* __restrict__ odd, const bf16x8* q, const Sees& sees,
+                                          int kend, float scale2, Running<HD>& run) {
+  constexpr int KB = BN / 32, DB = HD / 32;
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  if (more) {
+    const uint16_t *kc[Source<HD, WAVES, BN>::LOADS], *vc[Source<HD, WAVES, BN>::LOADS];
+    from.chunks(t + 1, kc, vc);
+    AMK_LDS uint16_t* to = next + threadIdx.x / 64 * 512;
+#pragma unroll
+    for (int i = 0; i < Source<HD, WAVES, BN>::LOADS; ++i) {
+      load_lds16(kc[i], to + i * WAVES * 512);
+      load_lds16(vc[i], to + i * WAVES * 512 + BN * HD);
+    }
+  }
+
+  f32x16 sc[KB] = {};
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) {
+      const int r = kb * 32 + col;
+      const bf16x8 kf = *(const AMK_LDS bf16x8*)(kt + r * HD + ((2 * i + half) ^ k_swizzle<HD>(r)) * 8);
+      sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
+    }
+
+  if constexpr (PARTIAL) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const uint32_t word = sees.word(t * BN + kb * 32, kend) >> 4 * half;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(word >> (8 * (i / 4) + i % 4) & 1)) sc[kb][i] = -INFINITY;
+    }
+  }
+
+  float top = -INFINITY;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float m_new = fmaxf(run.m, top * scale2);
+  const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: p = 2^-inf = 0
+  const float keep = __builtin_amdgcn_exp2f(run.m - base);
+  run.m = m_new;
+  float sum = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], scale2, -base));
+      sum += sc[kb][i];
+    }
+  run.l = run.l * keep + sum;
+  if (__any(keep != 1.f)) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) run.o[d][i] *= keep;
+  }
+
+  if constexpr (PARTIAL) {
+#pragma unroll
+    for (int i = 0; i < Source<HD, WAVES, BN>::LOADS; ++i) {
+      AMK_LDS u32x4* at = (AMK_LDS u32x4*)vt + i * 64 * WAVES + threadIdx.x;
+      u32x4 x = *at;
+      bool here = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool lo = (x[e] & 0x7f80u) == 0x7f80u, hi = (x[e] & 0x7f800000u) == 0x7f800000u;
+        here |= lo | hi;
+        x[e] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+      }
+      if (here) *at = x;
+      if (here) *odd = 1;
+    }
+    __syncthreads();
+    run.odd |= *odd;
+  }
+
+  bf16x8 p[KB][2];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[kb][i / 8][i % 8] = (__bf16)sc[kb][i];
+  const int vr = 4 * half + (lane & 15) / 4;  // + multiples of 8
+  const int vc = ((lane >> 4) & 1) * 2 + (lane & 3) / 2, ve = (lane & 1) * 4;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const AMK_LDS uint16_t* at = vt + (kb * 32 + ks * 16 + vr) * HD + ((4 * d + vc) ^ v_swizzle<HD>(vr)) * 8 + ve;
+        const s16x4 lo = read_tr16(at), hi = read_tr16(at + 8 * HD);
+        const s16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        run.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), p[kb][ks], run.o[d], 0, 0, 0);
+      }
+}
+
 template <int HD, int WAVES, int BN, typename Which>
 __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, const Which w) {
-  constexpr int ROWS = 32 * WAVES, CPR = HD / 8, KB = BN / 32, DB = HD / 32;
-  constexpr int TILE = BN * HD;                      // elements of a K or V tile
-  constexpr int LOADS = TILE / 8 / (64 * WAVES);     // 16-byte loads per lane and tile
-  static_assert(LOADS >= 1 && TILE % (8 * 64 * WAVES) == 0, "whole loads");
-  constexpr int WEIGHTS = WAVES * 32 * BN;           // p of all waves, where products are taken key by key
-  __shared__ __align__(16) uint16_t lds[2][2][TILE];  // [stage][K, V]
-  __shared__ __align__(16) uint16_t more[WEIGHTS > TILE ? WEIGHTS : 8];
+  constexpr int ROWS = 32 * WAVES, DB = HD / 32;
+  constexpr int TILE = BN * HD;  // elements of a K or V tile
+  // two stages of K and V and a flag: one variable, since the compiler keeps what it knows
+  // of attn_step's pointers only where a kernel has no second one
+  __shared__ __align__(16) uint16_t lds[4 * TILE + 8];
+  AMK_LDS uint16_t* stages = (AMK_LDS uint16_t*)lds;
+  AMK_LDS int* odd = (AMK_LDS int*)(stages + 4 * TILE);
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int half = lane >> 5, col = lane & 31;
@@ -186,153 +338,44 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
 
   const int ktiles = (kend + BN - 1) / BN;
   const int t0 = (int)((int64_t)ktiles * split / a.splits), t1 = (int)((int64_t)ktiles * (split + 1) / a.splits);
-  const uint16_t* kp = a.k + s.k0 * a.k_token + kvh * a.k_head;
-  const uint16_t* vp = a.v + s.k0 * a.v_token + kvh * a.v_head;
-  // this lane's chunk of a tile's first rows; later rows of a load follow STEP apart
-  constexpr int STEP = 64 * WAVES / CPR;
-  const int lr = threadIdx.x / CPR, lc = threadIdx.x % CPR;
-  const int vc0 = (lc ^ v_swizzle<HD>(lr)) * 8;
-  static_assert(STEP % 4 == 0, "V rows of a lane share their permutation");
-
-  auto load_tile = [&](int t, int stage) {
-    uint16_t* to = &lds[stage][0][wave * 512];
-    if (t * BN + BN <= s.nk) {
-      const uint16_t* kl = kp + (int64_t)(t * BN) * a.k_token + lr * a.k_token;
-      const uint16_t* vl = vp + (int64_t)(t * BN) * a.v_token + lr * a.v_token + vc0;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int kc = (lc ^ k_swizzle<HD>(lr + i * STEP)) * 8;
-        load_lds16(kl + i * STEP * a.k_token + kc, to + i * WAVES * 512);
-        load_lds16(vl + i * STEP * a.v_token, to + i * WAVES * 512 + TILE);
-      }
-    } else {  // rows past the last key repeat it: in range, and masked
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int kc = (lc ^ k_swizzle<HD>(lr + i * STEP)) * 8;
-        const int64_t key = min(t * BN + i * STEP + lr, s.nk - 1);
-        load_lds16(kp + key * a.k_token + kc, to + i * WAVES * 512);
-        load_lds16(vp + key * a.v_token + vc0, to + i * WAVES * 512 + TILE);
-      }
-    }
-  };
-
-  f32x16 o[DB] = {};
-  float m = -INFINITY, l = 0.f;
-
-  // one tile of keys; PARTIAL: some row sees only some of them
-  auto step = [&](const int t, auto partial) {
-    constexpr bool PARTIAL = decltype(partial)::value;
-    const int stage = (t - t0) & 1;
+  const int tf = max(t0, min(t1, kfull / BN));  // tiles that every row sees whole
+  const Source<HD, WAVES, BN> from = {a.k + s.k0 * a.k_token + kvh * a.k_head, a.v + s.k0 * a.v_token + kvh * a.v_head,
+                                      a.k_token, a.v_token, s.nk};
+  if (threadIdx.x == 0) *odd = 0;
+  Running<HD> run = {};
+  run.m = -INFINITY;
+  if (t0 < t1) from.tile(t0, stages);
+  int t = t0, stage = 0;
+  for (; t < tf; ++t, stage ^= 1) {
     wait_loads();
-    __syncthreads();  // this tile's loads are in, the other stage's readers are done
-    if (t + 1 < t1) load_tile(t + 1, stage ^ 1);
-    const uint16_t* kt = lds[stage][0];
-    const uint16_t* vt = lds[stage][1];
+    __syncthreads();  // tile t is in, and the readers of the other stage are done
+    AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
+    attn_step<HD, WAVES, BN, false>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE,
+                                    odd, q, sees, kend, a.scale2, run);
+  }
+  for (; t < t1; ++t, stage ^= 1) {
+    wait_loads();
+    __syncthreads();
+    AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
+    attn_step<HD, WAVES, BN, true>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE, odd,
+                                   q, sees, kend, a.scale2, run);
+  }
 
-    f32x16 sc[KB] = {};
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) {
-        const int r = kb * 32 + col;
-        const bf16x8 kf = *(const bf16x8*)(kt + r * HD + ((2 * i + half) ^ k_swizzle<HD>(r)) * 8);
-        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
-      }
-
-    if constexpr (PARTIAL) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const uint32_t word = sees.word(t * BN + kb * 32, kend) >> 4 * half;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!(word >> (8 * (i / 4) + i % 4) & 1)) sc[kb][i] = -INFINITY;
-      }
-    }
-
-    float top = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m_new = fmaxf(m, top * a.scale2);
-    const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: p = 2^-inf = 0
-    const float keep = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    float sum = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], a.scale2, -base));
-        sum += sc[kb][i];
-      }
-    l = l * keep + sum;
-    if (__any(keep != 1.f)) {
+  if (run.odd) {  // rare: add what was set to 0 to the rows that see it
+    for (int key = tf * BN; key < min(t1 * BN, kend); ++key) {
+      if (!(sees.word(key, kend) & 1)) continue;
+      const uint16_t* vp = from.v + key * a.v_token + 4 * half;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+        for (int i = 0; i < 16; ++i) {
+          const float x = bf16_to_f32(vp[32 * d + 8 * (i / 4) + i % 4]);
+          if (!(fabsf(x) < INFINITY)) run.o[d][i] += x;
+        }
     }
+  }
 
-    bf16x8 p[KB][2];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[kb][i / 8][i % 8] = (__bf16)sc[kb][i];
-
-    bool odd = false;
-    if constexpr (PARTIAL) {
-      for (int c = threadIdx.x; c < TILE / 8; c += 64 * WAVES) {
-        const u32x4 x = *(const u32x4*)(vt + c * 8);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
-      }
-      odd = __syncthreads_or(odd);
-    }
-    if (!odd) {
-      const int vr = 4 * half + (lane & 15) / 4;  // + multiples of 8
-      const int vc = ((lane >> 4) & 1) * 2 + (lane & 3) / 2, ve = (lane & 1) * 4;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const uint16_t* at = vt + (kb * 32 + ks * 16 + vr) * HD + ((4 * d + vc) ^ v_swizzle<HD>(vr)) * 8 + ve;
-            const s16x4 lo = read_tr16(at), hi = read_tr16(at + 8 * HD);
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const s16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), p[kb][ks], o[d], 0, 0, 0);
-          }
-    } else {
-      // key by key: the weights go through the K tile, which every wave has read, if they fit
-      uint16_t* pt = (WEIGHTS > TILE ? more : lds[stage][0]) + (wave * 32 + col) * BN;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) pt[kb * 32 + 8 * (i / 4) + 4 * half + i % 4] = f32_to_bf16(sc[kb][i]);
-      __syncthreads();
-      for (int j = 0; j < BN; ++j) {
-        if (!(sees.word(t * BN + j, kend) & 1)) continue;
-        const float pj = bf16_to_f32(pt[j]);
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int e = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-            o[d][i] += pj * bf16_to_f32(vt[j * HD + ((e / 8) ^ v_swizzle<HD>(j)) * 8 + e % 8]);
-          }
-      }
-    }
-  };
-  const int tf = max(t0, min(t1, kfull / BN));  // tiles that every row sees whole
-  if (t0 < t1) load_tile(t0, 0);
-  for (int t = t0; t < tf; ++t) step(t, std::false_type());
-  for (int t = tf; t < t1; ++t) step(t, std::true_type());
-
-  l += __shfl_xor(l, 32);
+  const float l = run.l + __shfl_xor(run.l, 32);
   if (!valid) return;
   if (a.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -341,19 +384,19 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32x2 v = {pack_bf16(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
-                         pack_bf16(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
+        const u32x2 v = {pack_bf16(run.o[d][4 * i] * inv, run.o[d][4 * i + 1] * inv),
+                         pack_bf16(run.o[d][4 * i + 2] * inv, run.o[d][4 * i + 3] * inv)};
         *(u32x2*)(op + 32 * d + 8 * i) = v;
       }
   } else {
     const int64_t at = ((int64_t)split * a.total_q + s.q0 + token) * a.n_heads + head;
-    if (half == 0) a.part_ml[at] = make_float2(m, l);
+    if (half == 0) a.part_ml[at] = make_float2(run.m, l);
     float* op = a.part_o + at * HD + 4 * half;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x4 v = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        const f32x4 v = {run.o[d][4 * i], run.o[d][4 * i + 1], run.o[d][4 * i + 2], run.o[d][4 * i + 3]};
         *(f32x4*)(op + 32 * d + 8 * i) = v;
       }
   }

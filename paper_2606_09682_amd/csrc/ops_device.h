@@ -11,6 +11,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -21,20 +22,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return (uint32_t)f32_to_bf16(lo) | (uint32_t)f32_to_bf16(hi) << 16;
 }
 
+#define AMK_LDS __attribute__((address_space(3)))
+
 // 16 bytes a lane from global memory into 1 KiB of LDS at `lds` (the same for
 // all lanes of the wave): lane i's bytes go to lds + 16 i.
-__device__ __forceinline__ void load_lds16(const void* g, void* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
-                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+__device__ __forceinline__ void load_lds16(const void* g, AMK_LDS void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, lds, 16, 0, 0);
 }
 
-// Waits for this wave's loads, those to LDS among them.
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits for this wave's loads, those to LDS among them (a barrier alone does not):
+// vmcnt 0, the other counters at their maximum.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // Transposed LDS read: in each 16 lanes, lane i addresses 4 elements of row i / 4
 // of a 4 x 16 block (columns 4 (i % 4) ..) and receives the block's column i.
-__device__ __forceinline__ s16x4 read_tr16(const void* lds) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds);
+__device__ __forceinline__ s16x4 read_tr16(const AMK_LDS uint16_t* lds) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((AMK_LDS s16x4*)lds);
 }
 
 }  // namespace amk
