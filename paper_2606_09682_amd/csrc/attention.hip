@@ -402,32 +402,56 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   }
 }
 
-// Joins the splits of each (token, head): one wave each, HD / 64 elements a lane.
-// Splits that saw nothing for the row (l = 0) are left out.
+// Joins the splits of each (token, head), one wave each: HD / 4 lanes take a split's row
+// of O, so 2 or 4 splits are read side by side and 8 or 16 are on their way.  Splits
+// that saw nothing for the row (l = 0) are left out.
 template <int HD>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, const int32_t* cu_q, int32_t n_seqs) {
-  const int lane = threadIdx.x & 63;
+  constexpr int LANES = HD / 4, SIDE = 64 / LANES, AHEAD = 4;
+  const int lane = threadIdx.x & 63, sub = lane / LANES;
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.total_q * a.n_heads;
   if (at >= all) return;
   const int64_t token = at / a.n_heads;
   const int head = (int)(at % a.n_heads);
   if (cu_q && (token < cu_q[0] || token >= cu_q[n_seqs])) return;
   float m = -INFINITY;
-  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, a.part_ml[i * all + at].x);
+  for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, a.part_ml[i * all + at].x);
+  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   const float base = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[HD / 64] = {};
-  for (int i = 0; i < a.splits; ++i) {
-    const float2 ml = a.part_ml[i * all + at];
-    if (ml.y == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - base);
-    l += f * ml.y;
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const float* po = a.part_o + at * HD + lane % LANES * 4;
+  for (int i0 = 0; i0 < a.splits; i0 += 64) {
+    float f = 0.f;
+    if (i0 + lane < a.splits) {
+      const float2 ml = a.part_ml[(i0 + lane) * all + at];
+      if (ml.y != 0.f) f = __builtin_amdgcn_exp2f(ml.x - base);
+      l += f * ml.y;
+    }
+    const int n = min(64, a.splits - i0);
+    for (int i = 0; i < n; i += SIDE * AHEAD) {
+      f32x4 v[AHEAD];
+      float w[AHEAD];
 #pragma unroll
-    for (int e = 0; e < HD / 64; ++e) o[e] += f * a.part_o[(i * all + at) * HD + lane * (HD / 64) + e];
+      for (int u = 0; u < AHEAD; ++u) {
+        const int k = i + u * SIDE + sub;
+        w[u] = __shfl(f, k & 63);
+        if (k >= n) w[u] = 0.f;
+        v[u] = *(const f32x4*)(po + (int64_t)(i0 + min(k, n - 1)) * all * HD);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (w[u] != 0.f) o += w[u] * v[u];
+    }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* op = a.out + token * a.out_token + head * a.out_head + lane * (HD / 64);
+  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
 #pragma unroll
-  for (int e = 0; e < HD / 64; ++e) op[e] = f32_to_bf16(o[e] * inv);
+  for (int e = 0; e < 4; ++e)
+    for (int d = 32; d >= LANES; d >>= 1) o[e] += __shfl_xor(o[e], d);
+  if (sub) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const u32x2 r = {pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+  *(u32x2*)(a.out + token * a.out_token + head * a.out_head + lane * 4) = r;
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -439,6 +463,9 @@ AttnPlan with_workspace(AttnPlan p, int n_heads, int head_dim, int total_q) {
 }
 
 constexpr int kSplitBlocks = 1024;  // workgroups that splits of the keys may add up to
+
+// Workgroups that run at once: each CU has registers for 8 waves.
+int resident(int waves) { return 256 * 8 / waves; }
 
 int waves_for(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
@@ -480,15 +507,19 @@ int launch_attn(const AttnArgs& r, const AttnPlan& p, int head_dim, const Which&
 
 }  // namespace
 
+// Splits of the keys: as many workgroups as run at once, if every one has `least` keys.
+int splits_for(int64_t blocks, int waves, int64_t keys, int least) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kSplitBlocks, resident(waves)) / blocks,
+                                                     (keys + least - 1) / least));
+}
+
 AttnPlan prompt_plan(int n_heads, int n_kv_heads, int head_dim, int n_seqs, int total_q, int total_k) {
   AttnPlan p;
   const int64_t rows = (int64_t)total_q * (n_heads / n_kv_heads);
   p.waves = waves_for(rows);
   // whole tiles of the sum, and one that is not whole per sequence
   p.tiles = (int)(rows / (32 * p.waves) + std::min<int64_t>(n_seqs, rows));
-  const int64_t blocks = (int64_t)p.tiles * n_kv_heads;
-  // few row tiles leave CUs without work: split their keys, in ranges of 256 at least
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitBlocks / 2 / blocks, ((int64_t)total_k + 255) / 256));
+  p.splits = splits_for((int64_t)p.tiles * n_kv_heads, p.waves, total_k, 256);
   return with_workspace(p, n_heads, head_dim, total_q);
 }
 
@@ -497,9 +528,7 @@ AttnPlan tree_plan(int n_heads, int n_kv_heads, int head_dim, int n, int pos) {
   const int64_t rows = (int64_t)n * (n_heads / n_kv_heads);
   p.waves = waves_for(rows);
   p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  const int64_t blocks = (int64_t)p.tiles * n_kv_heads;
-  // about kSplitBlocks workgroups, of 128 keys at least
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitBlocks / blocks, ((int64_t)pos + n + 127) / 128));
+  p.splits = splits_for((int64_t)p.tiles * n_kv_heads, p.waves, (int64_t)pos + n, 128);
   return with_workspace(p, n_heads, head_dim, n);
 }
 
