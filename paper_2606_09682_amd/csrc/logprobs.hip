@@ -13,8 +13,10 @@
 // entries reach, and few more do unless many are equal.  The entries that reach
 // it are listed and ranked by counting.  Where they overflow the list (rows of
 // few distinct values), `top` rounds each find the best entry after the last.
-// Entries compare by value and then the lower index, so the result is one and
-// the same however the list was filled.
+// An entry is a 64-bit key, the value's order above the inverted index, so that
+// larger keys come first and equal values by the lower index: the result is the
+// same however the list was filled.
+#include <algorithm>
 #include <cmath>
 
 #include "ops.h"
@@ -24,16 +26,20 @@ namespace amk {
 namespace {
 
 constexpr int NT = 512, WAVES = NT / 64;
+constexpr int NJ = 256;     // threads of the joining kernel
 constexpr int LIST = 1024;  // entries ranked by counting
 
-struct Best {
-  float x;
-  int32_t i;  // -1: none
-};
+typedef unsigned long long Key;  // 0: none
 
-// Whether a comes before b: the larger value, the lower index.
-__device__ __forceinline__ bool before(const Best& a, const Best& b) {
-  return a.i >= 0 && (b.i < 0 || a.x > b.x || (a.x == b.x && a.i < b.i));
+__device__ __forceinline__ Key key_of(float x, int i) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.f);  // one zero
+  const uint32_t order = b & 0x80000000u ? ~b : b | 0x80000000u;
+  return (Key)order << 32 | (uint32_t)~i;
+}
+__device__ __forceinline__ int index_of(Key k) { return ~(int)(uint32_t)k; }
+__device__ __forceinline__ float value_of(Key k) {
+  const uint32_t order = (uint32_t)(k >> 32);
+  return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
 }
 
 template <int TYPE>
@@ -57,220 +63,212 @@ struct Elem<AMK_F16> {
   static __device__ __forceinline__ float bits(uint32_t v) { return get((uint16_t)v); }
 };
 
-// The workgroup's maximum (NaN left out) and sum; every thread gets them.
-__device__ float block_max(float v, float* tmp) {
+__device__ __forceinline__ float wave_max(float v) {
   for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = tmp[0];
-  for (int i = 1; i < WAVES; ++i) v = fmaxf(v, tmp[i]);
   return v;
 }
-__device__ float block_sum(float v, float* tmp) {
+__device__ __forceinline__ float wave_sum(float v) {
   for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = tmp[0];
-  for (int i = 1; i < WAVES; ++i) v += tmp[i];
+  return v;
+}
+__device__ __forceinline__ Key wave_max(Key v) {
+  for (int d = 32; d; d >>= 1) v = max(v, (Key)__shfl_xor(v, d));
   return v;
 }
 
-// Ranks `count` listed entries and writes the best `top` in order (none: i = -1).
-__device__ void rank_list(const Best* list, int count, int top, Best* out) {
-  for (int c = threadIdx.x; c < count; c += NT) {
-    const Best b = list[c];
+// Writes the best `top` of the `count` listed keys in order, 0 where there are fewer.
+template <int THREADS>
+__device__ __forceinline__ void rank_list(const Key* list, int count, int top, Key* out) {
+  for (int c = threadIdx.x; c < count; c += THREADS) {
+    const Key k = list[c];
     int rank = 0;
-    for (int o = 0; o < count; ++o) rank += before(list[o], b);
-    if (b.i >= 0 && rank < top) out[rank] = b;
+#pragma unroll 8
+    for (int o = 0; o < count; ++o) rank += list[o] > k;
+    if (k && rank < top) out[rank] = k;
   }
+  for (int r = count + threadIdx.x; r < top; r += THREADS) out[r] = 0;
 }
 
-// The statistics of one chunk, then its best entries.
+// Maximum and sums of one chunk; s is NaN where the chunk holds a NaN or plus infinity.
 struct ChunkStat {
   float m, s, u;
-  int32_t nan;
 };
 
 template <int TYPE, int PER>
-__global__ void __launch_bounds__(NT) logprob_chunk_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
-                                                           int vocab, int chunks, int top, ChunkStat* stats,
-                                                           Best* best) {
+__global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
+                                                              int vocab, int chunks, int top, ChunkStat* stats,
+                                                              Key* best) {
   typedef typename Elem<TYPE>::T T;
   constexpr int VEC = 16 / sizeof(T);
-  __shared__ float tmp[WAVES];
   __shared__ float lane_max[WAVES][64];
-  __shared__ Best list[LIST];
-  __shared__ Best out[AMK_TOP_MAX];
+  __shared__ float2 sums[WAVES];
+  __shared__ Key list[LIST];
   __shared__ int count;
   __shared__ float reach;
-  __shared__ Best found[WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
   const T* p = logits + (int64_t)row * row_stride;
   // chunks are cut at 16-byte boundaries of memory: `skew` entries before the row
   const int skew = (int)(((uintptr_t)p & 15) / sizeof(T));
-  const int first = chunk * (NT * PER) - skew;
+  const int first = chunk * (NT * PER) - skew + (int)threadIdx.x * VEC;  // entry of x[0]
+  auto entry = [&](int j) { return first + j / VEC * (NT * VEC) + j % VEC; };
 
   float x[PER];
-  int at0[PER / VEC];
 #pragma unroll
-  for (int j = 0; j < PER / VEC; ++j) {
-    const int i = first + (j * NT + (int)threadIdx.x) * VEC;
-    at0[j] = i;
+  for (int j = 0; j < PER; j += VEC) {
+    const int i = entry(j);
     if (i >= 0 && i + VEC <= vocab) {
       const u32x4 v = *(const u32x4*)(p + i);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const uint32_t word = v[sizeof(T) == 4 ? e % 4 : e / 2 % 4];
-        x[j * VEC + e] = Elem<TYPE>::bits(sizeof(T) == 4 ? word : word >> (e % 2 * 16));
+        x[j + e] = Elem<TYPE>::bits(sizeof(T) == 4 ? word : word >> (e % 2 * 16));
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        x[j * VEC + e] = i + e >= 0 && i + e < vocab ? Elem<TYPE>::get(p[i + e]) : -INFINITY;
+      for (int e = 0; e < VEC; ++e) x[j + e] = i + e >= 0 && i + e < vocab ? Elem<TYPE>::get(p[i + e]) : -INFINITY;
     }
   }
-
-  float mine = -INFINITY;
-  bool nan = false;
+  float mine = x[0];
+#pragma unroll
+  for (int j = 1; j < PER; ++j) mine = fmaxf(mine, x[j]);  // NaN left out
+  lane_max[wave][lane] = mine;
+  if (threadIdx.x == 0) {
+    count = 0;
+    reach = -INFINITY;
+  }
+  __syncthreads();
+  float group = lane_max[0][lane];  // of this lane in all waves
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) group = fmaxf(group, lane_max[i][lane]);
+  const float m = wave_max(group);
+  if (top && wave == 0) {
+    int rank = 0;
+#pragma unroll
+    for (int o = 0; o < 64; ++o) {
+      const float v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), o));
+      rank += v > group || (v == group && o < lane);
+    }
+    if (rank == top - 1) reach = group;
+  }
+  // a NaN makes s NaN, and so does plus infinity (its own difference from m)
+  const float base = m == -INFINITY ? 0.f : m;
+  float s = 0.f, u = 0.f;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    mine = fmaxf(mine, x[j]);
-    nan |= x[j] != x[j];
+    const float z = x[j] - base, e = __expf(z);
+    s += e;
+    u += fmaxf(z, -200.f) * e;  // e is 0 long before
   }
-  const float m = block_max(mine, tmp);
-  float s = 0.f, u = 0.f;
-  if (m > -INFINITY) {
+  s = wave_sum(s);
+  u = wave_sum(u);
+  if (lane == 0) sums[wave] = make_float2(s, u);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = sums[0].x;
+    u = sums[0].y;
+    for (int i = 1; i < WAVES; ++i) {
+      s += sums[i].x;
+      u += sums[i].y;
+    }
+    stats[blockIdx.x] = {m, s, u};
+  }
+  if (top == 0) return;
+
+  Key* to = best + (int64_t)blockIdx.x * top;
+  const float least = reach;
+  if (mine >= least) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const float z = x[j] - m, e = __expf(z);
-      s += e;
-      u += e > 0.f ? z * e : 0.f;
-    }
-  }
-  s = block_sum(s, tmp);
-  u = block_sum(u, tmp);
-  nan = __syncthreads_or(nan);
-  if (threadIdx.x == 0) stats[blockIdx.x] = {m, s, u, nan};
-  if (top == 0 || nan) return;
-
-  lane_max[wave][lane] = mine;
-  if (threadIdx.x < AMK_TOP_MAX) out[threadIdx.x] = {-INFINITY, -1};
-  if (threadIdx.x == 0) count = 0;
-  __syncthreads();
-  if (wave == 0) {
-    float g = lane_max[0][lane];
-    for (int i = 1; i < WAVES; ++i) g = fmaxf(g, lane_max[i][lane]);
-    int rank = 0;
-    for (int o = 0; o < 64; ++o) {
-      const float v = __shfl(g, o);
-      rank += v > g || (v == g && o < lane);
-    }
-    if (rank == top - 1) reach = g;
-  }
-  __syncthreads();
-  const float least = reach;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int i = at0[j / VEC] + j % VEC;
-    if (x[j] >= least && i >= 0 && i < vocab) {
-      const int c = atomicAdd(&count, 1);
-      if (c < LIST) list[c] = {x[j], i};
-    }
-  }
-  __syncthreads();
-  if (count <= LIST) {
-    rank_list(list, count, top, out);
-  } else {
-    Best last = {INFINITY, -1};
-    for (int r = 0; r < top; ++r) {
-      Best b = {-INFINITY, -1};
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const Best c = {x[j], at0[j / VEC] + j % VEC};
-        if (c.i >= 0 && c.i < vocab && (r == 0 || before(last, c)) && before(c, b)) b = c;
+      const int i = entry(j);
+      if (x[j] >= least && i >= 0 && i < vocab) {
+        const int c = atomicAdd(&count, 1);
+        if (c < LIST) list[c] = key_of(x[j], i);
       }
-      for (int d = 32; d; d >>= 1) {
-        const Best c = {__shfl_xor(b.x, d), __shfl_xor(b.i, d)};
-        if (before(c, b)) b = c;
-      }
-      if (lane == 0) found[wave] = b;
-      __syncthreads();
-      b = found[0];
-      for (int i = 1; i < WAVES; ++i)
-        if (before(found[i], b)) b = found[i];
-      if (threadIdx.x == 0) out[r] = b;
-      last = b;
-      __syncthreads();
-      if (b.i < 0) break;
     }
   }
   __syncthreads();
-  if (threadIdx.x < top) best[(int64_t)blockIdx.x * top + threadIdx.x] = out[threadIdx.x];
+  const int listed = count;
+  if (listed <= LIST) {
+    rank_list<NT>(list, listed, top, to);
+    return;
+  }
+  Key last = ~0ull;
+  for (int r = 0; r < top; ++r) {
+    Key k = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = entry(j);
+      const Key c = key_of(x[j], i);
+      if (i >= 0 && i < vocab && x[j] == x[j] && c < last) k = max(k, c);
+    }
+    k = wave_max(k);
+    __syncthreads();
+    if (lane == 0) list[wave] = k;
+    __syncthreads();
+    for (int i = 0; i < WAVES; ++i) k = max(k, list[i]);
+    if (threadIdx.x == 0) to[r] = k;
+    last = k;
+  }
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(NT) logprob_join_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
+__global__ void __launch_bounds__(NJ) logprob_join_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
                                                           int vocab, int chunks, int top, const ChunkStat* stats,
-                                                          const Best* best, const int32_t* tokens, float* logprob,
+                                                          const Key* best, const int32_t* tokens, float* logprob,
                                                           float* entropy, int32_t* top_ids, float* top_logprobs) {
-  __shared__ float tmp[WAVES];
-  __shared__ Best list[LIST];
-  __shared__ Best out[AMK_TOP_MAX];
-  const int row = blockIdx.x;
+  __shared__ Key list[LIST];
+  __shared__ Key out[AMK_TOP_MAX];
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  // list the chunks' entries, as many chunks at a time as the list holds beside the best so far
+  const int per = top ? (LIST - AMK_TOP_MAX) / top : 0;
+  const Key* from = best + (int64_t)row * chunks * top;
+  const int first = min(per, chunks) * top;
+  for (int i = threadIdx.x; i < first; i += NJ) list[i] = from[i];
+
+  // every wave joins the statistics by itself
   const ChunkStat* st = stats + (int64_t)row * chunks;
   float m = -INFINITY;
-  bool nan = false;
-  for (int c = threadIdx.x; c < chunks; c += NT) {
-    m = fmaxf(m, st[c].m);
-    nan |= st[c].nan != 0;
-  }
-  m = block_max(m, tmp);
-  nan = __syncthreads_or(nan) || m == INFINITY || m == -INFINITY;
+  for (int c = lane; c < chunks; c += 64) m = fmaxf(m, st[c].m);
+  m = wave_max(m);
   float s = 0.f, u = 0.f;
-  for (int c = threadIdx.x; c < chunks; c += NT) {
+  for (int c = lane; c < chunks; c += 64) {
     // a chunk's sums move to the row's maximum: x - m = (x - mc) + (mc - m)
-    if (st[c].m == -INFINITY) continue;
-    const float d = st[c].m - m, f = __expf(d);
-    s += st[c].s * f;
-    u += f > 0.f ? (st[c].u + d * st[c].s) * f : 0.f;
+    const ChunkStat k = st[c];
+    const bool none = k.m == -INFINITY && k.s == 0.f;
+    const float d = none ? 0.f : fmaxf(k.m - m, -200.f), f = __expf(d);
+    s += k.s * f;
+    u += (k.u + d * k.s) * f;
   }
-  s = block_sum(s, tmp);
-  u = block_sum(u, tmp);
+  s = wave_sum(s);
+  u = wave_sum(u);
+  const bool bad = !(s < INFINITY) || m == -INFINITY;  // NaN, plus infinity or nothing possible
   const float ls = logf(s), none = __builtin_nanf("");
   if (threadIdx.x == 0) {
-    if (entropy) entropy[row] = nan ? none : ls - u / s;
+    if (entropy) entropy[row] = bad ? none : ls - u / s;
     if (tokens) {
       const int t = tokens[row];
       float lp = none;
-      if (!nan && t >= 0 && t < vocab) lp = Elem<TYPE>::get(logits[row * row_stride + t]) - m - ls;
+      if (!bad && t >= 0 && t < vocab) lp = Elem<TYPE>::get(logits[row * row_stride + t]) - m - ls;
       logprob[row] = lp;
     }
   }
   if (top == 0) return;
-  if (threadIdx.x < AMK_TOP_MAX) out[threadIdx.x] = {none, -1};
-  int count = 0;
-  if (!nan) {
-    // list the chunks' entries, as many chunks at a time as the list holds beside the best so far
-    const int per = (LIST - AMK_TOP_MAX) / top;
-    for (int c0 = 0; c0 < chunks; c0 += per) {
-      const int n = min(per, chunks - c0) * top;
-      __syncthreads();
-      for (int i = threadIdx.x; i < n; i += NT) list[count + i] = best[((int64_t)row * chunks + c0) * top + i];
-      __syncthreads();
-      rank_list(list, count + n, top, out);
-      __syncthreads();
-      if (threadIdx.x < top) list[threadIdx.x] = out[threadIdx.x];
-      count = top;
-    }
+  __syncthreads();
+  rank_list<NJ>(list, first, top, out);
+  for (int c0 = per; c0 < chunks; c0 += per) {
+    const int n = min(per, chunks - c0) * top;
+    __syncthreads();
+    if (threadIdx.x < top) list[threadIdx.x] = out[threadIdx.x];
+    for (int i = threadIdx.x; i < n; i += NJ) list[top + i] = from[(int64_t)c0 * top + i];
+    __syncthreads();
+    rank_list<NJ>(list, top + n, top, out);
   }
   __syncthreads();
   if (threadIdx.x < top) {
-    const Best b = out[threadIdx.x];
-    top_ids[(int64_t)row * top + threadIdx.x] = b.i;
-    top_logprobs[(int64_t)row * top + threadIdx.x] = b.i < 0 ? none : b.x - m - ls;
+    const Key k = out[threadIdx.x];
+    top_ids[(int64_t)row * top + threadIdx.x] = bad ? -1 : index_of(k);
+    top_logprobs[(int64_t)row * top + threadIdx.x] = bad ? none : value_of(k) - m - ls;
   }
 }
 
@@ -280,7 +278,7 @@ void launch_type(const LogprobPlan& p, const void* logits, int64_t row_stride, i
                  hipStream_t st) {
   typedef typename Elem<TYPE>::T T;
   ChunkStat* stats = (ChunkStat*)workspace;
-  Best* best = (Best*)((char*)workspace + ((size_t)n * p.chunks * sizeof(ChunkStat) + 255) / 256 * 256);
+  Key* best = (Key*)((char*)workspace + ((size_t)n * p.chunks * sizeof(ChunkStat) + 255) / 256 * 256);
   const dim3 grid((unsigned)((int64_t)n * p.chunks));
   if (p.chunk == NT * 32)
     hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 32>), grid, dim3(NT), 0, st, (const T*)logits, row_stride, vocab,
@@ -288,7 +286,7 @@ void launch_type(const LogprobPlan& p, const void* logits, int64_t row_stride, i
   else
     hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 8>), grid, dim3(NT), 0, st, (const T*)logits, row_stride, vocab,
                        p.chunks, top, stats, best);
-  hipLaunchKernelGGL(logprob_join_kernel<TYPE>, dim3(n), dim3(NT), 0, st, (const T*)logits, row_stride, vocab, p.chunks,
+  hipLaunchKernelGGL(logprob_join_kernel<TYPE>, dim3(n), dim3(NJ), 0, st, (const T*)logits, row_stride, vocab, p.chunks,
                      top, stats, best, tokens, logprob, entropy, top_ids, top_logprobs);
 }
 
@@ -305,7 +303,7 @@ LogprobPlan logprob_plan(int type, int n, int vocab, int top) {
     p.chunks = (vocab + skew + p.chunk - 1) / p.chunk;
   }
   const size_t all = (size_t)n * p.chunks;
-  p.workspace = (all * sizeof(ChunkStat) + 255) / 256 * 256 + all * top * sizeof(Best);
+  p.workspace = (all * sizeof(ChunkStat) + 255) / 256 * 256 + all * top * sizeof(Key);
   return p;
 }
 
