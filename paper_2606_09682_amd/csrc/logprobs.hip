@@ -25,9 +25,10 @@
 namespace amk {
 namespace {
 
-constexpr int NT = 512, WAVES = NT / 64;
+constexpr int NT = 256, WAVES = NT / 64;
 constexpr int NJ = 256;     // threads of the joining kernel
-constexpr int LIST = 1024;  // entries ranked by counting
+constexpr int LIST = 1024;  // keys ranked by counting
+constexpr int SEG = LIST / WAVES;  // of them, one wave's
 
 typedef unsigned long long Key;  // 0: none
 
@@ -76,17 +77,9 @@ __device__ __forceinline__ Key wave_max(Key v) {
   return v;
 }
 
-// Writes the best `top` of the `count` listed keys in order, 0 where there are fewer.
-template <int THREADS>
-__device__ __forceinline__ void rank_list(const Key* list, int count, int top, Key* out) {
-  for (int c = threadIdx.x; c < count; c += THREADS) {
-    const Key k = list[c];
-    int rank = 0;
-#pragma unroll 8
-    for (int o = 0; o < count; ++o) rank += list[o] > k;
-    if (k && rank < top) out[rank] = k;
-  }
-  for (int r = count + threadIdx.x; r < top; r += THREADS) out[r] = 0;
+__device__ __forceinline__ Key wave_min(Key v) {
+  for (int d = 32; d; d >>= 1) v = min(v, (Key)__shfl_xor(v, d));
+  return v;
 }
 
 // Maximum and sums of one chunk; s is NaN where the chunk holds a NaN or plus infinity.
@@ -102,8 +95,8 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
   constexpr int VEC = 16 / sizeof(T);
   __shared__ float lane_max[WAVES][64];
   __shared__ float2 sums[WAVES];
-  __shared__ Key list[LIST];
-  __shared__ int count;
+  __shared__ Key list[WAVES][SEG];
+  __shared__ int counts[WAVES];
   __shared__ float reach;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
@@ -129,27 +122,27 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
       for (int e = 0; e < VEC; ++e) x[j + e] = i + e >= 0 && i + e < vocab ? Elem<TYPE>::get(p[i + e]) : -INFINITY;
     }
   }
-  float mine = x[0];
+  // maxima of four entries each, then of all of the lane's (NaN left out)
+  float four[PER / 4], mine;
 #pragma unroll
-  for (int j = 1; j < PER; ++j) mine = fmaxf(mine, x[j]);  // NaN left out
-  lane_max[wave][lane] = mine;
-  if (threadIdx.x == 0) {
-    count = 0;
-    reach = -INFINITY;
+  for (int j = 0; j < PER / 4; ++j) {
+    four[j] = fmaxf(fmaxf(x[4 * j], x[4 * j + 1]), fmaxf(x[4 * j + 2], x[4 * j + 3]));
+    mine = j ? fmaxf(mine, four[j]) : four[j];
   }
+  lane_max[wave][lane] = mine;
   __syncthreads();
   float group = lane_max[0][lane];  // of this lane in all waves
 #pragma unroll
   for (int i = 1; i < WAVES; ++i) group = fmaxf(group, lane_max[i][lane]);
   const float m = wave_max(group);
   if (top && wave == 0) {
-    int rank = 0;
+    // the top-th largest value t: the least that fewer than `top` others exceed
+    int more = 0;
 #pragma unroll
-    for (int o = 0; o < 64; ++o) {
-      const float v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), o));
-      rank += v > group || (v == group && o < lane);
-    }
-    if (rank == top - 1) reach = group;
+    for (int o = 0; o < 64; ++o)
+      more += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), o)) > group;
+    const float t = -wave_max(more < top ? -group : -INFINITY);
+    if (lane == 0) reach = t;
   }
   // a NaN makes s NaN, and so does plus infinity (its own difference from m)
   const float base = m == -INFINITY ? 0.f : m;
@@ -177,20 +170,41 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
 
   Key* to = best + (int64_t)blockIdx.x * top;
   const float least = reach;
-  if (mine >= least) {
+  int count = 0;  // of the wave, in its own segment
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = entry(j);
-      if (x[j] >= least && i >= 0 && i < vocab) {
-        const int c = atomicAdd(&count, 1);
-        if (c < LIST) list[c] = key_of(x[j], i);
-      }
+  for (int j = 0; j < PER / 4; ++j) {
+    if (!__any(four[j] >= least)) continue;
+#pragma unroll
+    for (int e = 4 * j; e < 4 * j + 4; ++e) {
+      const int i = entry(e);
+      const bool in = x[e] >= least && i >= 0 && i < vocab;
+      const uint64_t lanes = __ballot(in);
+      const int at = count + __popcll(lanes & ((1ull << lane) - 1));
+      if (in && at < SEG) list[wave][at] = key_of(x[e], i);
+      count += __popcll(lanes);
     }
   }
+  if (lane == 0) counts[wave] = count;
   __syncthreads();
-  const int listed = count;
-  if (listed <= LIST) {
-    rank_list<NT>(list, listed, top, to);
+  int most = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    most = max(most, counts[w]);
+    all += counts[w];
+  }
+  if (most <= SEG) {
+    for (int c = lane; c < count; c += 64) {  // each wave ranks its own keys
+      const Key k = list[wave][c];
+      int rank = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const int n = counts[w];
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) rank += list[w][o] > k;
+      }
+      if (rank < top) to[rank] = k;
+    }
+    for (int r = all + threadIdx.x; r < top; r += NT) to[r] = 0;
     return;
   }
   Key last = ~0ull;
@@ -204,9 +218,9 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
     }
     k = wave_max(k);
     __syncthreads();
-    if (lane == 0) list[wave] = k;
+    if (lane == 0) list[wave][0] = k;
     __syncthreads();
-    for (int i = 0; i < WAVES; ++i) k = max(k, list[i]);
+    for (int w = 0; w < WAVES; ++w) k = max(k, list[w][0]);
     if (threadIdx.x == 0) to[r] = k;
     last = k;
   }
@@ -218,13 +232,10 @@ __global__ void __launch_bounds__(NJ) logprob_join_kernel(const typename Elem<TY
                                                           const Key* best, const int32_t* tokens, float* logprob,
                                                           float* entropy, int32_t* top_ids, float* top_logprobs) {
   __shared__ Key list[LIST];
-  __shared__ Key out[AMK_TOP_MAX];
+  __shared__ int count;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
-  // list the chunks' entries, as many chunks at a time as the list holds beside the best so far
-  const int per = top ? (LIST - AMK_TOP_MAX) / top : 0;
   const Key* from = best + (int64_t)row * chunks * top;
-  const int first = min(per, chunks) * top;
-  for (int i = threadIdx.x; i < first; i += NJ) list[i] = from[i];
+  if (threadIdx.x == 0) count = 0;
 
   // every wave joins the statistics by itself
   const ChunkStat* st = stats + (int64_t)row * chunks;
@@ -254,21 +265,52 @@ __global__ void __launch_bounds__(NJ) logprob_join_kernel(const typename Elem<TY
     }
   }
   if (top == 0) return;
+
+  // The chunks' lists are in order, so the first q of each make `top` keys that are at
+  // least the least of their q-th: keys below that are out, and few are left to rank.
+  const int q = (top + chunks - 1) / chunks;
+  Key least = ~0ull;
+  for (int c = lane; c < chunks; c += 64) least = min(least, from[c * top + q - 1]);
+  least = wave_min(least);
   __syncthreads();
-  rank_list<NJ>(list, first, top, out);
-  for (int c0 = per; c0 < chunks; c0 += per) {
-    const int n = min(per, chunks - c0) * top;
-    __syncthreads();
-    if (threadIdx.x < top) list[threadIdx.x] = out[threadIdx.x];
-    for (int i = threadIdx.x; i < n; i += NJ) list[top + i] = from[(int64_t)c0 * top + i];
-    __syncthreads();
-    rank_list<NJ>(list, top + n, top, out);
+  const int keys = chunks * top;
+  for (int i = threadIdx.x; i < keys; i += NJ) {
+    const Key k = from[i];
+    if (k && k >= least) {
+      const int at = atomicAdd(&count, 1);
+      if (at < LIST) list[at] = k;
+    }
   }
   __syncthreads();
-  if (threadIdx.x < top) {
-    const Key k = out[threadIdx.x];
-    top_ids[(int64_t)row * top + threadIdx.x] = bad ? -1 : index_of(k);
-    top_logprobs[(int64_t)row * top + threadIdx.x] = bad ? none : value_of(k) - m - ls;
+  const int listed = count;
+  auto put = [&](int r, Key k) {
+    top_ids[(int64_t)row * top + r] = bad || !k ? -1 : index_of(k);
+    top_logprobs[(int64_t)row * top + r] = bad || !k ? none : value_of(k) - m - ls;
+  };
+  if (listed <= LIST) {
+    for (int c = threadIdx.x; c < listed; c += NJ) {
+      const Key k = list[c];
+      int rank = 0;
+#pragma unroll 4
+      for (int o = 0; o < listed; ++o) rank += list[o] > k;
+      if (rank < top) put(rank, k);
+    }
+    for (int r = listed + threadIdx.x; r < top; r += NJ) put(r, 0);
+    return;
+  }
+  // too many equal candidates: the best after the last, `top` times
+  Key last = ~0ull;
+  for (int r = 0; r < top; ++r) {
+    Key k = 0;
+    for (int i = threadIdx.x; i < keys; i += NJ)
+      if (from[i] < last) k = max(k, from[i]);
+    k = wave_max(k);
+    __syncthreads();
+    if (lane == 0) list[threadIdx.x / 64] = k;
+    __syncthreads();
+    for (int w = 0; w < NJ / 64; ++w) k = max(k, list[w]);
+    if (threadIdx.x == 0) put(r, k);
+    last = k;
   }
 }
 
