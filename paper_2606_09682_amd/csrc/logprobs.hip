@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
   for (int j = 0; j < PER; j += VEC) {
     const int i = entry(j);
     if (i >= 0 && i + VEC <= vocab) {
-      const u32x4 v = *(const u32x4*)(p + i);
+      const u32x4 v = __builtin_nontemporal_load((const u32x4*)(p + i));
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const uint32_t word = v[sizeof(T) == 4 ? e % 4 : e / 2 % 4];
@@ -192,19 +192,34 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
     most = max(most, counts[w]);
     all += counts[w];
   }
+  if (all <= 64) {  // the usual case: one wave ranks them from its registers
+    if (wave) return;
+    int w = 0, at = lane;
+#pragma unroll
+    for (int i = 0; i + 1 < WAVES; ++i)
+      if (w == i && at >= counts[i]) {
+        at -= counts[i];
+        ++w;
+      }
+    const Key k = lane < all ? list[w][at] : 0;
+    int rank = 0;
+    for (int o = 0; o < all; ++o) {
+      const Key other = (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), o) << 32 |
+                        (uint32_t)__builtin_amdgcn_readlane((int)k, o);
+      rank += other > k;
+    }
+    if (lane < all && rank < top) to[rank] = k;
+    if (lane >= all && lane < top) to[lane] = 0;
+    return;
+  }
   if (most <= SEG) {
     for (int c = lane; c < count; c += 64) {  // each wave ranks its own keys
       const Key k = list[wave][c];
       int rank = 0;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        const int n = counts[w];
-#pragma unroll 4
-        for (int o = 0; o < n; ++o) rank += list[w][o] > k;
-      }
+      for (int w = 0; w < WAVES; ++w)
+        for (int o = 0; o < counts[w]; ++o) rank += list[w][o] > k;
       if (rank < top) to[rank] = k;
     }
-    for (int r = all + threadIdx.x; r < top; r += NT) to[r] = 0;
     return;
   }
   Key last = ~0ull;
