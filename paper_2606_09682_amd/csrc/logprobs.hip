@@ -64,20 +64,12 @@ struct Elem<AMK_F16> {
   static __device__ __forceinline__ float bits(uint32_t v) { return get((uint16_t)v); }
 };
 
-__device__ __forceinline__ float wave_max(float v) {
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-__device__ __forceinline__ Key wave_max(Key v) {
+__device__ __forceinline__ Key best_of_wave(Key v) {
   for (int d = 32; d; d >>= 1) v = max(v, (Key)__shfl_xor(v, d));
   return v;
 }
 
-__device__ __forceinline__ Key wave_min(Key v) {
+__device__ __forceinline__ Key least_of_wave(Key v) {
   for (int d = 32; d; d >>= 1) v = min(v, (Key)__shfl_xor(v, d));
   return v;
 }
@@ -88,7 +80,7 @@ struct ChunkStat {
 };
 
 template <int TYPE, int PER>
-__global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
+__global__ void __launch_bounds__(NT, 5) logprob_chunk_kernel(const typename Elem<TYPE>::T* logits, int64_t row_stride,
                                                               int vocab, int chunks, int top, ChunkStat* stats,
                                                               Key* best) {
   typedef typename Elem<TYPE>::T T;
@@ -97,7 +89,7 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
   __shared__ float2 sums[WAVES];
   __shared__ Key list[WAVES][SEG];
   __shared__ int counts[WAVES];
-  __shared__ float reach;
+  __shared__ int exceeds[WAVES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
   const T* p = logits + (int64_t)row * row_stride;
@@ -135,14 +127,13 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
 #pragma unroll
   for (int i = 1; i < WAVES; ++i) group = fmaxf(group, lane_max[i][lane]);
   const float m = wave_max(group);
-  if (top && wave == 0) {
-    // the top-th largest value t: the least that fewer than `top` others exceed
+  if (top) {  // how many of the 64 exceed this lane's, a share of them counted by each wave
     int more = 0;
 #pragma unroll
-    for (int o = 0; o < 64; ++o)
-      more += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), o)) > group;
-    const float t = -wave_max(more < top ? -group : -INFINITY);
-    if (lane == 0) reach = t;
+    for (int o = 0; o < 64 / WAVES; ++o)
+      more += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group),
+                                                                  wave * (64 / WAVES) + o)) > group;
+    exceeds[wave][lane] = more;
   }
   // a NaN makes s NaN, and so does plus infinity (its own difference from m)
   const float base = m == -INFINITY ? 0.f : m;
@@ -169,16 +160,22 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
   if (top == 0) return;
 
   Key* to = best + (int64_t)blockIdx.x * top;
-  const float least = reach;
-  int count = 0;  // of the wave, in its own segment
+  // the top-th largest of the 64: the least that fewer than `top` exceed
+  int more = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) more += exceeds[w][lane];
+  const float least = -wave_max(more < top ? -group : -INFINITY);
+  const bool inside = least > -INFINITY;  // entries outside the row are minus infinity
+  int count = 0;                          // of the wave, in its own segment
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) {
     if (!__any(four[j] >= least)) continue;
 #pragma unroll
     for (int e = 4 * j; e < 4 * j + 4; ++e) {
       const int i = entry(e);
-      const bool in = x[e] >= least && i >= 0 && i < vocab;
+      const bool in = x[e] >= least && (inside || (i >= 0 && i < vocab));
       const uint64_t lanes = __ballot(in);
+      if (!lanes) continue;
       const int at = count + __popcll(lanes & ((1ull << lane) - 1));
       if (in && at < SEG) list[wave][at] = key_of(x[e], i);
       count += __popcll(lanes);
@@ -194,7 +191,7 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
   }
   if (all <= 64) {  // the usual case: one wave ranks them from its registers
     if (wave) return;
-    int w = 0, at = lane;
+    int w = 0, at = lane;  // this lane's key: the at-th of segment w
 #pragma unroll
     for (int i = 0; i + 1 < WAVES; ++i)
       if (w == i && at >= counts[i]) {
@@ -231,7 +228,7 @@ __global__ void __launch_bounds__(NT, 4) logprob_chunk_kernel(const typename Ele
       const Key c = key_of(x[j], i);
       if (i >= 0 && i < vocab && x[j] == x[j] && c < last) k = max(k, c);
     }
-    k = wave_max(k);
+    k = best_of_wave(k);
     __syncthreads();
     if (lane == 0) list[wave][0] = k;
     __syncthreads();
@@ -286,7 +283,7 @@ __global__ void __launch_bounds__(NJ) logprob_join_kernel(const typename Elem<TY
   const int q = (top + chunks - 1) / chunks;
   Key least = ~0ull;
   for (int c = lane; c < chunks; c += 64) least = min(least, from[c * top + q - 1]);
-  least = wave_min(least);
+  least = least_of_wave(least);
   __syncthreads();
   const int keys = chunks * top;
   for (int i = threadIdx.x; i < keys; i += NJ) {
@@ -319,7 +316,7 @@ __global__ void __launch_bounds__(NJ) logprob_join_kernel(const typename Elem<TY
     Key k = 0;
     for (int i = threadIdx.x; i < keys; i += NJ)
       if (from[i] < last) k = max(k, from[i]);
-    k = wave_max(k);
+    k = best_of_wave(k);
     __syncthreads();
     if (lane == 0) list[threadIdx.x / 64] = k;
     __syncthreads();

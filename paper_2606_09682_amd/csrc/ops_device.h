@@ -40,4 +40,28 @@ __device__ __forceinline__ s16x4 read_tr16(const AMK_LDS uint16_t* lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((AMK_LDS s16x4*)lds);
 }
 
+// Reductions over a wave's 64 lanes in six steps within registers: shifts within rows of
+// 16 lanes, then the rows' last lanes passed on.  Every lane gets the result.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float identity, float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, identity),
+                                                               __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <typename Op>
+__device__ __forceinline__ float wave_reduce(float v, float identity, Op op) {
+  v = op(v, dpp<0x111, 0xf>(identity, v));
+  v = op(v, dpp<0x112, 0xf>(identity, v));
+  v = op(v, dpp<0x114, 0xf>(identity, v));
+  v = op(v, dpp<0x118, 0xf>(identity, v));
+  v = op(v, dpp<0x142, 0xa>(identity, v));
+  v = op(v, dpp<0x143, 0xc>(identity, v));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_reduce(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_reduce(v, 0.f, [](float a, float b) { return a + b; });
+}
+
 }  // namespace amk
