@@ -308,7 +308,8 @@ int amk_read_probe(const void* buf, int64_t bytes, int32_t blocks, uint32_t* sin
 enum { AMK_F32 = 0, AMK_BF16 = 1, AMK_F16 = 2 };
 
 /* y = x W^T (accumulate 0) or y += x W^T (accumulate 1) for n tokens.
- *   x: bf16 [n][in], rows x_stride apart (x and x_stride * 2 bytes 16-byte aligned)
+ *   x: bf16 [n][in], rows x_stride apart (x and x_stride * 2 bytes 16-byte aligned); in
+ *      and x_stride are at most 2^22
  *   w, scale: W [out][in] in weight_format, as under amk_linear_t (group_size as in
  *             amk_config_t); in is a multiple of 16, under W4A16 of 32 and of the group
  *   y: fp32 (y_type AMK_F32) or bf16 (AMK_BF16) [n][out], rows y_stride >= out apart

@@ -347,14 +347,14 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   if (t0 < t1) from.tile(t0, stages);
   int t = t0, stage = 0;
   for (; t < tf; ++t, stage ^= 1) {
-    wait_loads();
+    wait_loads<0>();
     __syncthreads();  // tile t is in, and the readers of the other stage are done
     AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
     attn_step<HD, WAVES, BN, false>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE,
                                     odd, q, sees, kend, a.scale2, run);
   }
   for (; t < t1; ++t, stage ^= 1) {
-    wait_loads();
+    wait_loads<0>();
     __syncthreads();
     AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
     attn_step<HD, WAVES, BN, true>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE, odd,

@@ -21,6 +21,8 @@
 // through LDS at the end.  Long prompts need large tiles, few reads of LDS a product
 // (KG 1); few tokens need the weights streamed by every CU, so small tiles and many
 // waves on their columns.
+#include <type_traits>
+
 #include "ops.h"
 #include "ops_device.h"
 
@@ -44,17 +46,25 @@ __device__ __forceinline__ bf16x8 int8_to_bf16(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// The 8 codes of one packed int4 word: low nibbles are columns 0..3, high ones 4..7.
+// The 8 codes of one packed int4 word (low nibbles are columns 0..3, high ones 4..7) as
+// (c + 8) * 2^-9: a byte 0..15 read as FP8 E4M3 is that number of steps of its subnormals.
+// Half the work of a conversion through fp32; the 8 comes off as a product with kEight.
 __device__ __forceinline__ bf16x8 int4_to_bf16(uint32_t w) {
   const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   u32x4 r;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const uint32_t n = (p < 2 ? lo : hi) >> (p % 2 * 16);
-    r[p] = pack_exact((float)(n & 0xffu) - 8.f, (float)((n >> 8) & 0xffu) - 8.f);
-  }
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+  r[0] = __builtin_bit_cast(uint32_t, a);
+  r[1] = __builtin_bit_cast(uint32_t, b);
+  r[2] = __builtin_bit_cast(uint32_t, c);
+  r[3] = __builtin_bit_cast(uint32_t, d);
   return __builtin_bit_cast(bf16x8, r);
 }
+constexpr uint32_t kEight = 0xbc80bc80u;  // two bf16 of -8 * 2^-9
+constexpr float kStep = 512.f;            // 2^9, in the scales
 
 template <int FMT, int TB_, int RB_, int WT_, int WR_, int KG_, int BKW_>
 struct Tile {
@@ -79,43 +89,95 @@ __device__ __forceinline__ int swizzle(int row) {
   return row / (16 / C) % C;
 }
 
-// Loads one stage: columns k0 .. of the tile's rows.  Rows past the last repeat it and
-// columns past the last the first ones: in range, and their results are not used.
-template <int FMT, typename G>
-__device__ __forceinline__ void load_stage(const LinearArgs& a, int t0, int r0, int k0,
-                                           AMK_LDS unsigned char* to) {
-  AMK_LDS unsigned char* dst = to + threadIdx.x / 64 * 1024;
-#pragma unroll
-  for (int i = 0; i < G::XLOADS; ++i) {
-    const int c = i * G::THREADS + threadIdx.x, at = c % G::XC, row = c / G::XC % G::BT, kg = c / (G::XC * G::BT);
-    int k = k0 + kg * G::BKW + (at ^ swizzle<G::XC>(row)) * 8;
-    k = k < a.in ? k : 0;
-    load_lds16(a.x + (int64_t)min(t0 + row, a.n - 1) * a.x_stride + k, dst + i * G::THREADS * 16);
+// This lane's loads of a stage: its 16 bytes of each lie in row `row` of the tile, at
+// column `k` of the stage.
+template <typename G>
+struct Lane {
+  int row, k;
+  static __device__ __forceinline__ Lane x(int i) {
+    const int c = i * G::THREADS + threadIdx.x, row = c / G::XC % G::BT;
+    return {row, c / (G::XC * G::BT) * G::BKW + (c % G::XC ^ swizzle<G::XC>(row)) * 8};
   }
-#pragma unroll
-  for (int i = 0; i < G::WLOADS; ++i) {
-    const int c = i * G::THREADS + threadIdx.x, at = c % G::WC, row = c / G::WC % G::BR, kg = c / (G::WC * G::BR);
-    int k = k0 + kg * G::BKW + (at ^ swizzle<G::WC>(row)) * (128 / G::EIGHT);
-    k = k < a.in ? k : 0;
-    const int64_t eight = ((int64_t)min(r0 + row, a.out - 1) * a.in + k) / 8;
-    load_lds16((const unsigned char*)a.w + eight * G::EIGHT, dst + (G::XCHUNKS + i * G::THREADS) * 16);
+  static __device__ __forceinline__ Lane w(int i) {
+    const int c = i * G::THREADS + threadIdx.x, row = c / G::WC % G::BR;
+    return {row, c / (G::WC * G::BR) * G::BKW + (c % G::WC ^ swizzle<G::WC>(row)) * (128 / G::EIGHT)};
   }
-}
+};
 
-// The products of this wave's share of one stage.  xs, ws and next do not overlap: without
-// that promise every read would wait for the loads of the next stage.
+// The tile's first rows of x and W, and the bytes from there to the rows of this lane's
+// loads (rows past the last repeat it) at column 0 of a stage.
+template <typename G>
+struct Source {
+  const unsigned char *x, *w;
+  uint32_t xo[G::XLOADS], wo[G::WLOADS];
+
+  __device__ __forceinline__ Source(const LinearArgs& a, int t0, int r0) {
+    x = (const unsigned char*)(a.x + (int64_t)t0 * a.x_stride);
+    w = (const unsigned char*)a.w + (int64_t)r0 * (a.in / 8) * G::EIGHT;
+#pragma unroll
+    for (int i = 0; i < G::XLOADS; ++i) {
+      const Lane<G> l = Lane<G>::x(i);
+      xo[i] = (uint32_t)min(l.row, a.n - 1 - t0) * (uint32_t)a.x_stride * 2 + l.k * 2;
+    }
+#pragma unroll
+    for (int i = 0; i < G::WLOADS; ++i) {
+      const Lane<G> l = Lane<G>::w(i);
+      wo[i] = (uint32_t)min(l.row, a.out - 1 - r0) * (uint32_t)(a.in / 8) * G::EIGHT + l.k / 8 * G::EIGHT;
+    }
+  }
+
+  // Loads the stage of columns k0 ..; for columns past the last, which are not used, the first.
+  __device__ __forceinline__ void stage(int k0, int in, AMK_LDS unsigned char* to) const {
+    AMK_LDS unsigned char* dst = to + threadIdx.x / 64 * 1024;
+    const bool whole = k0 + G::COLS <= in;
+    const unsigned char *xs = x, *ws = w;
+    uint32_t xi[G::XLOADS], wi[G::WLOADS];
+#pragma unroll
+    for (int i = 0; i < G::XLOADS; ++i) xi[i] = xo[i];
+#pragma unroll
+    for (int i = 0; i < G::WLOADS; ++i) wi[i] = wo[i];
+    if (whole) {
+      xs += (int64_t)k0 * 2;
+      ws += (int64_t)(k0 / 8) * G::EIGHT;
+    } else {
+#pragma unroll
+      for (int i = 0; i < G::XLOADS; ++i) {
+        const int k = Lane<G>::x(i).k;
+        xi[i] = xi[i] - k * 2 + (k0 + k < in ? k0 + k : 0) * 2;
+      }
+#pragma unroll
+      for (int i = 0; i < G::WLOADS; ++i) {
+        const int k = Lane<G>::w(i).k;
+        wi[i] = wi[i] - k / 8 * G::EIGHT + (k0 + k < in ? k0 + k : 0) / 8 * G::EIGHT;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < G::XLOADS; ++i) load_lds16(xs + xi[i], dst + i * G::THREADS * 16);
+#pragma unroll
+    for (int i = 0; i < G::WLOADS; ++i) load_lds16(ws + wi[i], dst + (G::XCHUNKS + i * G::THREADS) * 16);
+  }
+};
+
+// The products of this wave's share of the stage of columns k0 .., while the one after it
+// (if more follow) is loaded into `next`.  xs, ws and next do not overlap: without that
+// promise every read would wait for the loads.  TAIL: columns past the last count as 0.
 template <int FMT, typename G, bool TAIL, bool GROUP32>
-__device__ __forceinline__ void linear_step(const LinearArgs& a, int t0, int r0, int k0, bool more,
+__device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k0, bool more,
                                             const AMK_LDS unsigned char* __restrict__ xs,
                                             const AMK_LDS unsigned char* __restrict__ ws,
                                             AMK_LDS unsigned char* __restrict__ next, const float (&scale)[G::RB][2],
-                                            f32x16 (&acc)[G::TB][G::RB], f32x16 (&part)[G::TB][G::RB]) {
+                                            f32x16 (&acc)[G::TB][G::RB]) {
+  constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
   const int kg = wave / (G::WT * G::WR), wt = wave % G::WT, wr = wave / G::WT % G::WR;
   const int kw = k0 + kg * G::BKW;  // the wave's first column
-  if (more) load_stage<FMT, G>(a, t0, r0, k0 + G::COLS, next);
+  if (more) from.stage(k0 + G::COLS, in, next);
   xs += (kg * G::BT + wt * 32 * G::TB + col) * G::XC * 16;
   ws += (kg * G::BR + wr * 32 * G::RB + col) * G::WC * 16;
+  const bf16x8 nothing = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  const bf16x8 eight = __builtin_bit_cast(bf16x8, u32x4{kEight, kEight, kEight, kEight});
+  // W4A16: the sums of a group of columns, and of 8 times x there (one for all rows of W)
+  f32x16 part[G::TB][G::RB], off[G::TB];
 #pragma unroll
   for (int u = 0; u < G::BKW / 32; ++u) {
     bf16x8 xf[G::TB][2], wf[G::RB][2];
@@ -123,9 +185,9 @@ __device__ __forceinline__ void linear_step(const LinearArgs& a, int t0, int r0,
     for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int row = 32 * tb + col, c = (4 * u + 2 * half + s) ^ swizzle<G::XC>(row);
+        const int c = (4 * u + 2 * half + s) ^ swizzle<G::XC>(32 * tb + col);
         xf[tb][s] = *(const AMK_LDS bf16x8*)(xs + 32 * tb * G::XC * 16 + c * 16);
-        if (TAIL && kw + 32 * u + 16 * half + 8 * s >= a.in) xf[tb][s] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+        if (TAIL && kw + 32 * u + 16 * half + 8 * s >= in) xf[tb][s] = nothing;
       }
 #pragma unroll
     for (int rb = 0; rb < G::RB; ++rb) {
@@ -143,50 +205,59 @@ __device__ __forceinline__ void linear_step(const LinearArgs& a, int t0, int r0,
         wf[rb][0] = int4_to_bf16(v[0]);
         wf[rb][1] = int4_to_bf16(v[1]);
       }
-    }
-    if constexpr (TAIL) {  // W's too: 0 times what lies there need not be 0
-#pragma unroll
-      for (int rb = 0; rb < G::RB; ++rb)
+      if constexpr (TAIL && !W4)  // 0 times what lies there need not be 0
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          if (kw + 32 * u + 16 * half + 8 * s >= a.in) wf[rb][s] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+          if (kw + 32 * u + 16 * half + 8 * s >= in) wf[rb][s] = nothing;
     }
-    f32x16(&sum)[G::TB][G::RB] = FMT == AMK_WEIGHTS_W4A16 ? part : acc;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
+      const bool first = W4 && s == 0 && (GROUP32 || u == 0);
 #pragma unroll
-      for (int tb = 0; tb < G::TB; ++tb)
+      for (int tb = 0; tb < G::TB; ++tb) {
 #pragma unroll
-        for (int rb = 0; rb < G::RB; ++rb)
-          sum[tb][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], wf[rb][s], sum[tb][rb], 0, 0, 0);
-    if constexpr (FMT == AMK_WEIGHTS_W4A16) {
-      // a group of columns is complete: at the end of the slice, where the next one is
-      // another's (column groups of waves), or at the group's end
-      const bool last = u + 1 == G::BKW / 32;
-      if (GROUP32 || (last && (G::KG > 1 || ((kw + G::BKW) & (a.group - 1)) == 0 || TAIL))) {
+        for (int rb = 0; rb < G::RB; ++rb) {
+          f32x16& sum = W4 ? part[tb][rb] : acc[tb][rb];
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], wf[rb][s], first ? f32x16{} : sum, 0, 0, 0);
+        }
+        if constexpr (W4) {
+          f32x16& sum = G::RB == 1 ? part[tb][0] : off[tb];
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], eight, first && G::RB > 1 ? f32x16{} : sum, 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (W4) {
+      if (GROUP32 || u + 1 == G::BKW / 32) {
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
           for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              acc[tb][rb][i] = __builtin_fmaf(scale[rb][GROUP32 ? u : 0], part[tb][rb][i], acc[tb][rb][i]);
-              part[tb][rb][i] = 0.f;
-            }
+            for (int e = 0; e < 16; ++e)
+              acc[tb][rb][e] = __builtin_fmaf(scale[rb][GROUP32 ? u : 0],
+                                              G::RB == 1 ? part[tb][rb][e] : part[tb][rb][e] + off[tb][e],
+                                              acc[tb][rb][e]);
       }
     }
   }
 }
 
-__device__ __forceinline__ void put(const LinearArgs& a, int t, int r, float y) {
-  const int64_t at = t * a.y_stride + r;
-  if (a.y_bf16) {
+template <bool BF16, bool ADD>
+__device__ __forceinline__ void put(const LinearArgs& a, int64_t at, float y) {
+  if (BF16) {
     uint16_t* p = (uint16_t*)a.y + at;
-    *p = f32_to_bf16(a.accumulate ? bf16_to_f32(*p) + y : y);
+    *p = f32_to_bf16(ADD ? bf16_to_f32(*p) + y : y);
   } else {
     float* p = (float*)a.y + at;
-    *p = a.accumulate ? *p + y : y;
+    *p = ADD ? *p + y : y;
   }
+}
+
+// Calls f with the kind of output as constants.
+template <typename F>
+__device__ __forceinline__ void by_output(const LinearArgs& a, F f) {
+  if (a.y_bf16) a.accumulate ? f(std::true_type(), std::true_type()) : f(std::true_type(), std::false_type());
+  else a.accumulate ? f(std::false_type(), std::true_type()) : f(std::false_type(), std::false_type());
 }
 
 template <int FMT, typename G, bool GROUP32>
@@ -202,73 +273,63 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
   if ((int)(blockIdx.x / 8) >= each || tile >= tiles) return;
   const int t0 = tile % token_tiles * G::BT, r0 = tile / token_tiles * G::BR;
 
-  // this lane's rows of W and, under W4A16, their scales of the next stage's groups
+  // under W4A16: this lane's rows of the scales, and the scales of its wave's next slice
+  constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
+  const int groups = W4 ? a.in / a.group : 0, shift = W4 ? __builtin_ctz(a.group) : 0;
   const uint16_t* srow[G::RB];
-  const int groups = FMT == AMK_WEIGHTS_W4A16 ? a.in / a.group : 0;
+  uint16_t ahead[G::RB][2];
 #pragma unroll
   for (int rb = 0; rb < G::RB; ++rb)
     srow[rb] = (const uint16_t*)a.scale + (int64_t)min(r0 + (wr * G::RB + rb) * 32 + col, a.out - 1) * groups;
-  const int shift = FMT == AMK_WEIGHTS_W4A16 ? __builtin_ctz(a.group) : 0;
-  uint16_t ahead[G::RB][2] = {};
   auto fetch = [&](int k0) {
-    if constexpr (FMT == AMK_WEIGHTS_W4A16) {
-      const int kw = k0 + kg * G::BKW;
+    if constexpr (W4)
 #pragma unroll
       for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
         for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u)
-          ahead[rb][u] = srow[rb][min((kw + 32 * u) >> shift, groups - 1)];
-    }
+          ahead[rb][u] = srow[rb][min((k0 + kg * G::BKW + 32 * u) >> shift, groups - 1)];
   };
 
-  f32x16 acc[G::TB][G::RB] = {}, part[G::TB][G::RB] = {};
+  f32x16 acc[G::TB][G::RB] = {};
+  const Source<G> from(a, t0, r0);
   fetch(0);
-  load_stage<FMT, G>(a, t0, r0, 0, mem);
-  int stage = 0, k0 = 0;
-  for (; k0 + G::COLS <= a.in; k0 += G::COLS, stage ^= 1) {
-    wait_loads();
+  from.stage(0, a.in, mem);
+  int k0 = 0, slot = 0;
+  auto take = [&](auto tail) {
+    wait_loads<0>();
     __syncthreads();  // the stage is in, and the readers of the other one are done
     float scale[G::RB][2] = {};
-    if constexpr (FMT == AMK_WEIGHTS_W4A16) {
+    if constexpr (W4) {
 #pragma unroll
       for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) scale[rb][u] = half_to_f32(ahead[rb][u]);
-      fetch(k0 + G::COLS);
+        for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u) scale[rb][u] = half_to_f32(ahead[rb][u]) * kStep;
     }
-    AMK_LDS unsigned char* cur = mem + stage * G::STAGE;
-    linear_step<FMT, G, false, GROUP32>(a, t0, r0, k0, k0 + G::COLS < a.in, cur, cur + 16 * G::XCHUNKS,
-                                        mem + (stage ^ 1) * G::STAGE, scale, acc, part);
-  }
-  if (k0 < a.in) {
-    wait_loads();
-    __syncthreads();
-    float scale[G::RB][2] = {};
-    if constexpr (FMT == AMK_WEIGHTS_W4A16) {
-#pragma unroll
-      for (int rb = 0; rb < G::RB; ++rb)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) scale[rb][u] = half_to_f32(ahead[rb][u]);
-    }
-    AMK_LDS unsigned char* cur = mem + stage * G::STAGE;
-    linear_step<FMT, G, true, GROUP32>(a, t0, r0, k0, false, cur, cur + 16 * G::XCHUNKS, mem + (stage ^ 1) * G::STAGE,
-                                       scale, acc, part);
-  }
+    const bool more = k0 + G::COLS < a.in;
+    if (more) fetch(k0 + G::COLS);
+    AMK_LDS unsigned char* cur = mem + slot * G::STAGE;
+    linear_step<FMT, G, decltype(tail)::value, GROUP32>(from, a.in, k0, more, cur, cur + 16 * G::XCHUNKS,
+                                                        mem + (slot ^ 1) * G::STAGE, scale, acc);
+  };
+  for (; k0 + G::COLS <= a.in; k0 += G::COLS, slot ^= 1) take(std::false_type());
+  if (k0 < a.in) take(std::true_type());
 
   if constexpr (G::KG == 1) {
+    by_output(a, [&](auto bf16, auto add) {
 #pragma unroll
-    for (int rb = 0; rb < G::RB; ++rb) {
-      const int r = r0 + (wr * G::RB + rb) * 32 + col;
-      if (r >= a.out) continue;
-      const float sc = FMT == AMK_WEIGHTS_W8A16 ? ((const float*)a.scale)[r] : 1.f;
+      for (int rb = 0; rb < G::RB; ++rb) {
+        const int r = r0 + (wr * G::RB + rb) * 32 + col;
+        if (r >= a.out) continue;
+        const float sc = FMT == AMK_WEIGHTS_W8A16 ? ((const float*)a.scale)[r] : 1.f;
 #pragma unroll
-      for (int tb = 0; tb < G::TB; ++tb)
+        for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = t0 + (wt * G::TB + tb) * 32 + 8 * (i / 4) + 4 * half + i % 4;
-          if (t < a.n) put(a, t, r, acc[tb][rb][i] * sc);
-        }
-    }
+          for (int e = 0; e < 16; ++e) {
+            const int t = t0 + (wt * G::TB + tb) * 32 + 8 * (e / 4) + 4 * half + e % 4;
+            if (t < a.n) put<decltype(bf16)::value, decltype(add)::value>(a, t * a.y_stride + r, acc[tb][rb][e] * sc);
+          }
+      }
+    });
   } else {
     // add up the column groups in order
     constexpr int BLOCKS = G::TB * G::RB;
@@ -279,17 +340,23 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
 #pragma unroll
       for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sums[((kg * BLOCKS + tb * G::RB + rb) * 16 + i) * 64 + lane] = acc[tb][rb][i];
+        for (int e = 0; e < 16; ++e)
+          sums[((kg * BLOCKS + tb * G::RB + rb) * 16 + e) * 64 + lane] = acc[tb][rb][e];
     __syncthreads();
-    for (int o = threadIdx.x; o < BLOCKS * 1024; o += G::THREADS) {
-      const int l = o % 64, i = o / 64 % 16, rb = o / 1024 % G::RB, tb = o / 1024 / G::RB;
-      const int t = t0 + tb * 32 + 8 * (i / 4) + 4 * (l / 32) + i % 4, r = r0 + rb * 32 + l % 32;
-      if (t >= a.n || r >= a.out) continue;
-      float y = sums[o];
-      for (int g = 1; g < G::KG; ++g) y += sums[g * BLOCKS * 1024 + o];
-      put(a, t, r, FMT == AMK_WEIGHTS_W8A16 ? y * ((const float*)a.scale)[r] : y);
-    }
+    by_output(a, [&](auto bf16, auto add) {
+#pragma unroll
+      for (int n = 0; n < BLOCKS * 1024 / G::THREADS; ++n) {
+        const int o = n * G::THREADS + threadIdx.x;
+        const int l = o % 64, e = o / 64 % 16, rb = o / 1024 % G::RB, tb = o / 1024 / G::RB;
+        const int t = t0 + tb * 32 + 8 * (e / 4) + 4 * (l / 32) + e % 4, r = r0 + rb * 32 + l % 32;
+        if (t >= a.n || r >= a.out) continue;
+        float y = sums[o];
+#pragma unroll
+        for (int g = 1; g < G::KG; ++g) y += sums[g * BLOCKS * 1024 + o];
+        if (FMT == AMK_WEIGHTS_W8A16) y *= ((const float*)a.scale)[r];
+        put<decltype(bf16)::value, decltype(add)::value>(a, t * a.y_stride + r, y);
+      }
+    });
   }
 }
 
@@ -307,10 +374,15 @@ int launch_tile(const LinearArgs& a, hipStream_t st) {
 template <int FMT>
 int launch_fmt(const LinearArgs& a, hipStream_t st) {
   constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
-  const int64_t large = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
   if (a.n <= 32) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32>>(a, st);
-  if (large < 128) return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
-  return launch_tile<FMT, Tile<FMT, W4 ? 2 : 4, 2, 2, 4, 1, 64>>(a, st);
+  const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
+  const int64_t t128 = (int64_t)((a.n + 127) / 128) * ((a.out + 127) / 128);
+  if (t128 < 128) return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+  // the time of whole rounds of tiles: a 256 x 256 tile to a CU, or two of 128 x 128, which
+  // take about 0.6 of its time together
+  const int64_t large = (t256 + 255) / 256 * 10, medium = (t128 + 511) / 512 * 6;
+  if (large <= medium) return launch_tile<FMT, Tile<FMT, W4 ? 2 : 4, 2, 2, 4, 1, 64>>(a, st);
+  return launch_tile<FMT, Tile<FMT, 2, 2, 2, 2, 1, 64>>(a, st);
 }
 
 }  // namespace

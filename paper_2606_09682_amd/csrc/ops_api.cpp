@@ -49,7 +49,7 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
   const bool w4 = weight_format == AMK_WEIGHTS_W4A16;
   const int group = group_size ? group_size : 128;
   if (w4 && (group < 32 || group > 1024 || (group & (group - 1)))) return AMK_ERR_INVALID_ARGUMENT;
-  if (in % 16 || (w4 && in % group)) return AMK_ERR_UNSUPPORTED;
+  if (in % 16 || (w4 && in % group) || in > 1 << 22 || x_stride > 1 << 22) return AMK_ERR_UNSUPPORTED;
   if (n == 0 || out == 0) return AMK_OK;
   if (!x || !w || !y || !aligned(x, 16) || !aligned(w, 16) || x_stride < in || x_stride % 8 || y_stride < out ||
       !aligned(y, y_type == AMK_F32 ? 4 : 2))

@@ -30,9 +30,13 @@ __device__ __forceinline__ void load_lds16(const void* g, AMK_LDS void* lds) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, lds, 16, 0, 0);
 }
 
-// Waits for this wave's loads, those to LDS among them (a barrier alone does not):
-// vmcnt 0, the other counters at their maximum.
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// Waits until at most N of this wave's loads, those to LDS among them, are under way
+// (a barrier alone does not): they return in order.  The other counters stay at their maximum.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "the counter has 6 bits");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
 
 // Transposed LDS read: in each 16 lanes, lane i addresses 4 elements of row i / 4
 // of a 4 x 16 block (columns 4 (i % 4) ..) and receives the block's column i.
