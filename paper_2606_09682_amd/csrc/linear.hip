@@ -66,21 +66,23 @@ __device__ __forceinline__ bf16x8 int4_to_bf16(uint32_t w) {
 constexpr uint32_t kEight = 0xbc80bc80u;  // two bf16 of -8 * 2^-9
 constexpr float kStep = 512.f;            // 2^9, in the scales
 
-template <int FMT, int TB_, int RB_, int WT_, int WR_, int KG_, int BKW_>
+template <int FMT, int TB_, int RB_, int WT_, int WR_, int KG_, int BKW_, int STAGES_ = 2, int XR_ = 32 * TB_ * WT_>
 struct Tile {
   static constexpr int TB = TB_, RB = RB_, WT = WT_, WR = WR_, KG = KG_, BKW = BKW_;
+  static constexpr int STAGES = STAGES_, XR = XR_;            // ring of stages, rows of x in each
   static constexpr int WAVES = WT * WR * KG, THREADS = 64 * WAVES;
   static constexpr int BT = 32 * TB * WT, BR = 32 * RB * WR;  // tokens, rows of W
   static constexpr int COLS = KG * BKW;                       // columns of a stage
   static constexpr int EIGHT = FMT == AMK_WEIGHTS_BF16 ? 16 : FMT == AMK_WEIGHTS_W8A16 ? 8 : 4;  // bytes of 8 columns of W
   static constexpr int XC = BKW / 8, WC = BKW * EIGHT / 128;  // 16-byte chunks per row of a slice
-  static constexpr int XCHUNKS = KG * BT * XC, WCHUNKS = KG * BR * WC;
+  static constexpr int XCHUNKS = KG * XR * XC, WCHUNKS = KG * BR * WC;
   static constexpr int XLOADS = XCHUNKS / THREADS, WLOADS = WCHUNKS / THREADS;
   static constexpr int STAGE = 16 * (XCHUNKS + WCHUNKS);
   static constexpr int JOIN = KG > 1 ? KG * TB * RB * 4096 : 0;  // sums of all column groups
-  static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
+  static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
   static_assert(XCHUNKS % THREADS == 0 && WCHUNKS % THREADS == 0 && WLOADS > 0 && XLOADS > 0, "whole loads");
   static_assert(KG == 1 || (WT == 1 && WR == 1), "column groups share one tile");
+  static_assert(XR == BT || TB * WT == 1, "rows of x repeat in the only block of tokens");
 };
 
 // Permutation of the C chunks of a row: rows that share a bank row of 256 bytes differ.
@@ -95,8 +97,8 @@ template <typename G>
 struct Lane {
   int row, k;
   static __device__ __forceinline__ Lane x(int i) {
-    const int c = i * G::THREADS + threadIdx.x, row = c / G::XC % G::BT;
-    return {row, c / (G::XC * G::BT) * G::BKW + (c % G::XC ^ swizzle<G::XC>(row)) * 8};
+    const int c = i * G::THREADS + threadIdx.x, row = c / G::XC % G::XR;
+    return {row, c / (G::XC * G::XR) * G::BKW + (c % G::XC ^ swizzle<G::XC>(row)) * 8};
   }
   static __device__ __forceinline__ Lane w(int i) {
     const int c = i * G::THREADS + threadIdx.x, row = c / G::WC % G::BR;
@@ -158,8 +160,8 @@ struct Source {
   }
 };
 
-// The products of this wave's share of the stage of columns k0 .., while the one after it
-// (if more follow) is loaded into `next`.  xs, ws and next do not overlap: without that
+// The products of this wave's share of the stage of columns k0 .., while the one that
+// takes the place of the stage before (if more follow) is loaded into `next`.  xs, ws and next do not overlap: without that
 // promise every read would wait for the loads.  TAIL: columns past the last count as 0.
 template <int FMT, typename G, bool TAIL, bool GROUP32>
 __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k0, bool more,
@@ -171,8 +173,9 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
   const int kg = wave / (G::WT * G::WR), wt = wave % G::WT, wr = wave / G::WT % G::WR;
   const int kw = k0 + kg * G::BKW;  // the wave's first column
-  if (more) from.stage(k0 + G::COLS, in, next);
-  xs += (kg * G::BT + wt * 32 * G::TB + col) * G::XC * 16;
+  if (more) from.stage(k0 + (G::STAGES - 1) * G::COLS, in, next);
+  const int xrow = col % G::XR;  // few tokens: their rows repeat, and the results of the copies are left
+  xs += (kg * G::XR + wt * 32 * G::TB + xrow) * G::XC * 16;
   ws += (kg * G::BR + wr * 32 * G::RB + col) * G::WC * 16;
   const bf16x8 nothing = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   const bf16x8 eight = __builtin_bit_cast(bf16x8, u32x4{kEight, kEight, kEight, kEight});
@@ -185,7 +188,7 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
     for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int c = (4 * u + 2 * half + s) ^ swizzle<G::XC>(32 * tb + col);
+        const int c = (4 * u + 2 * half + s) ^ swizzle<G::XC>(32 * tb + xrow);
         xf[tb][s] = *(const AMK_LDS bf16x8*)(xs + 32 * tb * G::XC * 16 + c * 16);
         if (TAIL && kw + 32 * u + 16 * half + 8 * s >= in) xf[tb][s] = nothing;
       }
@@ -292,12 +295,19 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
 
   f32x16 acc[G::TB][G::RB] = {};
   const Source<G> from(a, t0, r0);
+  constexpr int AHEAD = G::STAGES - 1;  // stages under way behind the one in use
+  constexpr int LOADS = G::XLOADS + G::WLOADS;
+  static_assert(!W4 || AHEAD == 1, "scales are fetched one stage ahead: waiting for them is waiting for all");
   fetch(0);
-  from.stage(0, a.in, mem);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i * G::COLS < a.in) from.stage(i * G::COLS, a.in, mem + i * G::STAGE);
   int k0 = 0, slot = 0;
   auto take = [&](auto tail) {
-    wait_loads<0>();
-    __syncthreads();  // the stage is in, and the readers of the other one are done
+    // the stage is in once only the loads issued after its own are under way, and the
+    // readers of the stage before are done
+    if (k0 + AHEAD * G::COLS <= a.in) stage_barrier<(AHEAD - 1) * LOADS>();
+    else stage_barrier<0>();
     float scale[G::RB][2] = {};
     if constexpr (W4) {
 #pragma unroll
@@ -305,13 +315,14 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
 #pragma unroll
         for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u) scale[rb][u] = half_to_f32(ahead[rb][u]) * kStep;
     }
-    const bool more = k0 + G::COLS < a.in;
-    if (more) fetch(k0 + G::COLS);
-    AMK_LDS unsigned char* cur = mem + slot * G::STAGE;
-    linear_step<FMT, G, decltype(tail)::value, GROUP32>(from, a.in, k0, more, cur, cur + 16 * G::XCHUNKS,
-                                                        mem + (slot ^ 1) * G::STAGE, scale, acc);
+    fetch(k0 + G::COLS);
+    AMK_LDS unsigned char *cur = mem + slot * G::STAGE, *next = mem + (slot ? slot - 1 : AHEAD) * G::STAGE;
+    linear_step<FMT, G, decltype(tail)::value, GROUP32>(from, a.in, k0, k0 + AHEAD * G::COLS < a.in,
+                                                        cur, cur + 16 * G::XCHUNKS, next, scale, acc);
+    k0 += G::COLS;
+    slot = slot == AHEAD ? 0 : slot + 1;
   };
-  for (; k0 + G::COLS <= a.in; k0 += G::COLS, slot ^= 1) take(std::false_type());
+  while (k0 + G::COLS <= a.in) take(std::false_type());
   if (k0 < a.in) take(std::true_type());
 
   if constexpr (G::KG == 1) {
@@ -374,10 +385,21 @@ int launch_tile(const LinearArgs& a, hipStream_t st) {
 template <int FMT>
 int launch_fmt(const LinearArgs& a, hipStream_t st) {
   constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
-  if (a.n <= 32) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32>>(a, st);
-  const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
+  const int64_t t32 = (int64_t)((a.n + 31) / 32) * ((a.out + 31) / 32);
+  const int64_t t64 = (int64_t)((a.n + 63) / 64) * ((a.out + 63) / 64);
   const int64_t t128 = (int64_t)((a.n + 127) / 128) * ((a.out + 127) / 128);
-  if (t128 < 128) return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+  const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
+  // few tokens, padded to 16 only, a ring of three: 16 tokens bf16 4096 -> 4096 8.3 us, with two 11.5
+  if (a.n <= 16) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32, W4 ? 2 : 3, 16>>(a, st);
+  if (t128 < 256) {
+    // Not enough for large tiles: whole rounds of 32 x 32, two to a CU, or of 64 x 64, which
+    // load the same bytes in a round and half as many a product.  128 tokens int8 4096 -> 4096
+    // 14.0 us in one round of 32 x 32 (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336
+    // 34.3 us in one round of 64 x 64 (42.8 in two of 32 x 32).
+    if (a.n <= 32 || (t32 + 511) / 512 <= (t64 + 255) / 256)
+      return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+    return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+  }
   // the time of whole rounds of tiles: a 256 x 256 tile to a CU, or two of 128 x 128, which
   // take about 0.6 of its time together
   const int64_t large = (t256 + 255) / 256 * 10, medium = (t128 + 511) / 512 * 6;

@@ -38,6 +38,18 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
 }
 
+// The workgroup's barrier of a ring of stages: at most N loads of every wave are still
+// under way behind it, and no read of LDS.  (A barrier with a fence would wait for all
+// loads to LDS.)
+template <int N>
+__device__ __forceinline__ void stage_barrier() {
+  static_assert(N < 64, "the counter has 6 bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Transposed LDS read: in each 16 lanes, lane i addresses 4 elements of row i / 4
 // of a 4 x 16 block (columns 4 (i % 4) ..) and receives the block's column i.
 __device__ __forceinline__ s16x4 read_tr16(const AMK_LDS uint16_t* lds) {
