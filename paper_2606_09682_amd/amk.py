@@ -269,47 +269,55 @@ def amk_schedule_check(cfg: amk_config_t, n_cu: int, tasks, n_counters: int,
 # ---- operators for several tokens over torch device tensors ---------------------------
 # Each call runs on the tensors' device and torch's current stream there, on which its
 # outputs and workspaces are allocated too; nothing synchronises.  The library sees
-# bare pointers, so types, shapes, devices and strides are checked here.
+# bare pointers, so types, shapes, devices and strides are checked here.  Small calls
+# take the GPU a few microseconds, so what runs on every call is kept short: a stream
+# is read as its raw handle, and messages are made only for a refusal.
 _FORMATS = {"bf16": AMK_WEIGHTS_BF16, "w8a16": AMK_WEIGHTS_W8A16, "w4a16": AMK_WEIGHTS_W4A16}
+_torch = None
 
 
-def _tensor(t, what: str, device, dtypes, dim: int):
-    """Check one operand: a tensor of `dim` dimensions and one of `dtypes` on `device`."""
-    if t.device != device:
-        raise ValueError(f"{what} is on {t.device}, expected {device}")
+def _load_torch():
+    """torch (imported on first use), with the types and functions the calls use."""
+    global _torch, _BF16, _WEIGHT, _SCALE, _OUT, _LOGITS
+    import torch
+    _BF16 = (torch.bfloat16, torch.int16)  # int16: bf16 bits
+    _WEIGHT = (_BF16, (torch.int8,), (torch.uint8,))
+    _SCALE = ((), (torch.float32,), (torch.float16,))
+    _OUT = {torch.float32: AMK_F32, torch.bfloat16: AMK_BF16}
+    _LOGITS = {torch.float32: AMK_F32, torch.bfloat16: AMK_BF16, torch.float16: AMK_F16}
+    _torch = torch
+    return torch
+
+
+def _refuse(t, what: str, index: int, dtypes, dim: int):
+    if t.get_device() != index:
+        raise ValueError(f"{what} is on {t.device}, expected cuda:{index}")
     if t.dtype not in dtypes:
         raise ValueError(f"{what} has type {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-    if t.dim() != dim:
-        raise ValueError(f"{what} has {t.dim()} dimensions, expected {dim}")
-    return t
+    raise ValueError(f"{what} has {t.dim()} dimensions, expected {dim}")
 
 
-def _cuda(t, what: str):
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a device tensor")
-    return t.device
-
-
-def _stream(device) -> int:
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def _call(device, fn, *args) -> None:
-    """Run fn(*args) with `device` current and raise on an error status."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        status = fn(*args)
+def _call(index: int, fn, *args) -> None:
+    """fn(*args, stream) with device `index` current; raises on an error status."""
+    torch = _torch
+    if torch.cuda.current_device() == index:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
-        with torch.cuda.device(device):
-            status = fn(*args)
+        with torch.cuda.device(index):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     if status != AMK_OK:
         raise AmkError(status, fn.__name__)
 
 
-def _workspace(nbytes: int, device):
-    import torch
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _device_index(t, what: str) -> int:
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{what} must be a device tensor")
+    return index
+
+
+def _workspace(nbytes: int, index: int):
+    return _torch.empty(nbytes, dtype=_torch.uint8, device=_torch.device("cuda", index))
 
 
 def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, out=None, out_dtype=None,
@@ -319,74 +327,84 @@ def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, o
     fp32 scale [out]; packed uint8 [out, in / 2] with fp16 scale [out, in / group]).
     Returns [n, out] of out_dtype (fp32, the default, or bf16), or writes it to `out`
     (contiguous rows) and returns that; accumulate adds to `out`."""
-    import torch
-    if weight_format not in _FORMATS:
+    torch = _torch or _load_torch()
+    fmt = _FORMATS.get(weight_format)
+    if fmt is None:
         raise ValueError(f"unknown weight format {weight_format}")
-    fmt = _FORMATS[weight_format]
-    device = _cuda(x, "x")
-    _tensor(x, "x", device, (torch.bfloat16, torch.int16), 2)
+    index = _device_index(x, "x")
+    if x.dtype not in _BF16 or x.dim() != 2:
+        _refuse(x, "x", index, _BF16, 2)
+    if w.get_device() != index or w.dtype not in _WEIGHT[fmt] or w.dim() != 2:
+        _refuse(w, "w", index, _WEIGHT[fmt], 2)
     n, width = x.shape
+    rows, stored = w.shape
     if n and x.stride(1) != 1:
         raise ValueError("x must have contiguous rows")
-    w_types = {AMK_WEIGHTS_BF16: (torch.bfloat16, torch.int16), AMK_WEIGHTS_W8A16: (torch.int8,),
-               AMK_WEIGHTS_W4A16: (torch.uint8,)}[fmt]
-    _tensor(w, "w", device, w_types, 2)
-    rows = w.shape[0]
-    if not w.is_contiguous() or w.shape[1] * (2 if fmt == AMK_WEIGHTS_W4A16 else 1) != width:
+    if (stored * 2 if fmt == AMK_WEIGHTS_W4A16 else stored) != width or not w.is_contiguous():
         raise ValueError(f"w must be contiguous rows of {width} columns")
     scale_ptr = None
     if fmt != AMK_WEIGHTS_BF16:
         if scale is None:
             raise ValueError(f"{weight_format} weights need a scale")
         w4 = fmt == AMK_WEIGHTS_W4A16
-        _tensor(scale, "scale", device, (torch.float16,) if w4 else (torch.float32,), 2 if w4 else 1)
-        if not scale.is_contiguous() or scale.numel() != (rows * (width // (group_size or 128)) if w4 else rows):
+        if scale.get_device() != index or scale.dtype not in _SCALE[fmt] or scale.dim() != 1 + w4:
+            _refuse(scale, "scale", index, _SCALE[fmt], 1 + w4)
+        if scale.numel() != (rows * (width // (group_size or 128)) if w4 else rows) or not scale.is_contiguous():
             raise ValueError("scale must be contiguous, one value per row (and group of columns)")
         scale_ptr = scale.data_ptr()
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty(n, rows, dtype=out_dtype or torch.float32, device=device)
-    _tensor(out, "out", device, (torch.float32, torch.bfloat16) if out_dtype is None else (out_dtype,), 2)
-    if out.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("out must be float32 or bfloat16")
-    if tuple(out.shape) != (n, rows) or (out.numel() and out.stride(1) != 1):
-        raise ValueError(f"out must be [{n}, {rows}] with contiguous rows")
-    _call(device, load().amk_linear, x.data_ptr(), x.stride(0) if n > 1 else (width + 7) // 8 * 8, n, width, rows,
-          w.data_ptr(), scale_ptr, fmt, group_size, out.data_ptr(), out.stride(0) if n > 1 else rows,
-          AMK_F32 if out.dtype == torch.float32 else AMK_BF16, int(accumulate), _stream(device))
+        out_dtype = out_dtype or torch.float32
+        if out_dtype not in _OUT:
+            raise ValueError("out_dtype must be float32 or bfloat16")
+        out = torch.empty((n, rows), dtype=out_dtype, device=x.device)
+        y_stride = rows
+    else:
+        allowed = tuple(_OUT) if out_dtype is None else (out_dtype,)
+        if out.get_device() != index or out.dtype not in allowed or out.dtype not in _OUT or out.dim() != 2:
+            _refuse(out, "out", index, tuple(_OUT), 2)
+        if tuple(out.shape) != (n, rows) or (out.numel() and out.stride(1) != 1):
+            raise ValueError(f"out must be [{n}, {rows}] with contiguous rows")
+        y_stride = out.stride(0) if n > 1 else rows
+    _call(index, load().amk_linear, x.data_ptr(), x.stride(0) if n > 1 else (width + 7) // 8 * 8, n, width, rows,
+          w.data_ptr(), scale_ptr, fmt, group_size, out.data_ptr(), y_stride, _OUT[out.dtype], int(accumulate))
     return out
 
 
+def _strides(t, name: str):
+    """(token, head) strides of [tokens, heads, head_dim]; a dimension of one element is
+    not stepped over, so any stride will do for it."""
+    (tokens, heads, d), (token, head, one) = t.shape, t.stride()
+    if one != 1 and d > 1 and t.numel():
+        raise ValueError(f"{name} must have contiguous heads")
+    return token if tokens > 1 else 8, head if heads > 1 else 8
+
+
 def _attention(q, k, v, scale, out):
-    """(amk_attention_t, out) of operands [tokens, heads, head_dim] after checking them."""
-    import torch
-    device = _cuda(q, "q")
-    bf16 = (torch.bfloat16, torch.int16)
-    for t, what in ((q, "q"), (k, "k"), (v, "v")):
-        _tensor(t, what, device, bf16, 3)
+    """(amk_attention_t, out, device index) of operands [tokens, heads, head_dim] after checking them."""
+    torch = _torch or _load_torch()
+    index = _device_index(q, "q")
+    if q.dtype not in _BF16 or q.dim() != 3:
+        _refuse(q, "q", index, _BF16, 3)
+    if k.get_device() != index or k.dtype not in _BF16 or k.dim() != 3:
+        _refuse(k, "k", index, _BF16, 3)
+    if v.get_device() != index or v.dtype not in _BF16 or v.dim() != 3:
+        _refuse(v, "v", index, _BF16, 3)
     tokens, heads, d = q.shape
-    rows, kv_heads, _ = k.shape
     if k.shape != v.shape or k.shape[2] != d:
         raise ValueError("k and v must be [rows, kv heads, head_dim] with q's head_dim")
     if out is None:
-        out = torch.empty(tokens, heads, d, dtype=q.dtype, device=device)
+        out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
     else:
-        _tensor(out, "out", device, bf16, 3)
+        if out.get_device() != index or out.dtype not in _BF16 or out.dim() != 3:
+            _refuse(out, "out", index, _BF16, 3)
         if out.shape != q.shape:
             raise ValueError("out must have q's shape")
-    a = amk_attention_t()
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        token, head, one = t.stride()
-        if t.numel() and one != 1 and d > 1:
-            raise ValueError(f"{name} must have contiguous heads")
-        setattr(a, name, t.data_ptr() or None)
-        # a dimension of one element is not stepped over: any stride will do
-        setattr(a, name + "_token", token if t.shape[0] > 1 else 8)
-        setattr(a, name + "_head", head if t.shape[1] > 1 else 8)
-    a.n_heads, a.n_kv_heads, a.head_dim = heads, kv_heads, d
-    a.scale = 1.0 / d ** 0.5 if scale is None else scale
-    return a, out, device
+    a = amk_attention_t(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *_strides(q, "q"), *_strides(k, "k"),
+                        *_strides(v, "v"), *_strides(out, "out"), heads, k.shape[1], d,
+                        d ** -0.5 if scale is None else scale)
+    return a, out, index
 
 
 def prompt_attention(q, k, v, cu_q=None, cu_k=None, scale: Optional[float] = None, out=None):
@@ -395,23 +413,22 @@ def prompt_attention(q, k, v, cu_q=None, cu_k=None, scale: Optional[float] = Non
     heads (a cache layer kv[l, 0] is taken as kv[l, 0].transpose(0, 1)).  cu_q and
     cu_k: int32 device tensors [sequences + 1] of offsets, or both None for one
     sequence.  Rows of `out` outside every sequence are not written."""
-    import torch
-    a, out, device = _attention(q, k, v, scale, out)
+    a, out, index = _attention(q, k, v, scale, out)
     seqs, pq, pk = 1, None, None
     if (cu_q is None) != (cu_k is None):
         raise ValueError("cu_q and cu_k come together")
     if cu_q is not None:
         for t, what in ((cu_q, "cu_q"), (cu_k, "cu_k")):
-            _tensor(t, what, device, (torch.int32,), 1)
+            if t.get_device() != index or t.dtype != _torch.int32 or t.dim() != 1:
+                _refuse(t, what, index, (_torch.int32,), 1)
             if not t.is_contiguous() or t.numel() != cu_q.numel() or t.numel() < 1:
                 raise ValueError("cu_q and cu_k must be contiguous and of one length")
         seqs, pq, pk = cu_q.numel() - 1, cu_q.data_ptr(), cu_k.data_ptr()
     lib = load()
     tokens, rows = q.shape[0], k.shape[0]
     need = lib.amk_prompt_attention_workspace(a.n_heads, a.n_kv_heads, a.head_dim, seqs, tokens, rows)
-    ws = _workspace(need, device)
-    _call(device, lib.amk_prompt_attention, a, pq, pk, seqs, tokens, rows, ws.data_ptr() if need else None, need,
-          _stream(device))
+    ws = _workspace(need, index) if need else None
+    _call(index, lib.amk_prompt_attention, a, pq, pk, seqs, tokens, rows, ws.data_ptr() if need else None, need)
     return out
 
 
@@ -431,7 +448,7 @@ def tree_attention(q, k, v, pos: int, masks, scale: Optional[float] = None, out=
     heads, head_dim]; k and v [rows, kv heads, head_dim] as in prompt_attention, with
     at least pos + n rows; masks: n whole numbers, bit j of masks[i] set where token
     i sees row pos + j (tree_masks gives a tree's)."""
-    a, out, device = _attention(q, k, v, scale, out)
+    a, out, index = _attention(q, k, v, scale, out)
     n = q.shape[0]
     if len(masks) != n:
         raise ValueError(f"{len(masks)} masks for {n} tokens")
@@ -441,9 +458,8 @@ def tree_attention(q, k, v, pos: int, masks, scale: Optional[float] = None, out=
         raise ValueError(f"k and v have {k.shape[0]} rows, tokens at {pos} need {pos + n}")
     lib = load()
     need = lib.amk_tree_attention_workspace(a.n_heads, a.n_kv_heads, a.head_dim, n, pos)
-    ws = _workspace(need, device)
-    _call(device, lib.amk_tree_attention, a, n, pos, (ctypes.c_uint64 * n)(*masks), ws.data_ptr() if need else None,
-          need, _stream(device))
+    ws = _workspace(need, index) if need else None
+    _call(index, lib.amk_tree_attention, a, n, pos, (ctypes.c_uint64 * n)(*masks), ws.data_ptr() if need else None, need)
     return out
 
 
@@ -451,32 +467,34 @@ def token_logprobs(logits, tokens=None, top: int = 0):
     """(logprob, entropy, top_ids, top_logprobs) of rows of logits (amk_token_logprobs):
     logits fp32, bf16 or fp16 [n, vocab] with contiguous rows; tokens int32 [n], or
     None (logprob is then None); the `top` most probable tokens of each row."""
-    import torch
-    device = _cuda(logits, "logits")
-    types = {torch.float32: AMK_F32, torch.bfloat16: AMK_BF16, torch.float16: AMK_F16}
-    _tensor(logits, "logits", device, tuple(types), 2)
+    torch = _torch or _load_torch()
+    index = _device_index(logits, "logits")
+    kind = _LOGITS.get(logits.dtype)
+    if kind is None or logits.dim() != 2:
+        _refuse(logits, "logits", index, tuple(_LOGITS), 2)
     n, vocab = logits.shape
     if n and vocab > 1 and logits.stride(1) != 1:
         raise ValueError("logits must have contiguous rows")
     if not 0 <= top <= AMK_TOP_MAX:
         raise ValueError(f"top must be in [0, {AMK_TOP_MAX}]")
-    logprob = None
+    lib = load()
+    need = lib.amk_token_logprobs_workspace(kind, n, vocab, top)
+    device = logits.device
+    logprob = token_ptr = logprob_ptr = None
     if tokens is not None:
-        _tensor(tokens, "tokens", device, (torch.int32,), 1)
-        if not tokens.is_contiguous() or tokens.numel() != n:
+        if tokens.get_device() != index or tokens.dtype != torch.int32 or tokens.dim() != 1:
+            _refuse(tokens, "tokens", index, (torch.int32,), 1)
+        if tokens.numel() != n or not tokens.is_contiguous():
             raise ValueError(f"tokens must be {n} contiguous values")
         logprob = torch.empty(n, dtype=torch.float32, device=device)
+        token_ptr, logprob_ptr = tokens.data_ptr(), logprob.data_ptr()
     entropy = torch.empty(n, dtype=torch.float32, device=device)
-    ids = torch.empty(n, top, dtype=torch.int32, device=device)
-    values = torch.empty(n, top, dtype=torch.float32, device=device)
-    lib = load()
-    kind = types[logits.dtype]
-    need = lib.amk_token_logprobs_workspace(kind, n, vocab, top)
-    ws = _workspace(need, device)
-    _call(device, lib.amk_token_logprobs, logits.data_ptr(), kind, logits.stride(0) if n > 1 else vocab, n, vocab,
-          tokens.data_ptr() if logprob is not None else None, top, logprob.data_ptr() if logprob is not None else None,
-          entropy.data_ptr(), ids.data_ptr() if top else None, values.data_ptr() if top else None,
-          ws.data_ptr() if need else None, need, _stream(device))
+    ids = torch.empty((n, top), dtype=torch.int32, device=device)
+    values = torch.empty((n, top), dtype=torch.float32, device=device)
+    ws = _workspace(need, index) if need else None
+    _call(index, lib.amk_token_logprobs, logits.data_ptr(), kind, logits.stride(0) if n > 1 else vocab, n, vocab,
+          token_ptr, top, logprob_ptr, entropy.data_ptr(), ids.data_ptr() if top else None,
+          values.data_ptr() if top else None, ws.data_ptr() if need else None, need)
     return logprob, entropy, ids, values
 
 
@@ -484,13 +502,14 @@ def kv_keep(kv, pos: int, rows) -> None:
     """Move cache rows pos + rows[i] to pos + i in every layer and head (amk_kv_keep):
     kv a contiguous 2-byte tensor [layers, 2, kv heads, max_seq, head_dim], rows
     strictly ascending whole numbers."""
-    device = _cuda(kv, "kv")
+    if _torch is None:
+        _load_torch()
+    index = _device_index(kv, "kv")
     if kv.dim() != 5 or kv.shape[1] != 2 or kv.element_size() != 2 or not kv.is_contiguous():
         raise ValueError("kv must be a contiguous bf16 tensor [layers, 2, kv heads, max_seq, head_dim]")
     layers, _, heads, cap, d = kv.shape
     n = len(rows)
-    _call(device, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n,
-          _stream(device))
+    _call(index, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n)
 
 
 # ---- convenience: a decoder over torch device tensors ---------------------------------
@@ -635,6 +654,7 @@ class Decoder:
             raise ValueError(f"n_logits must be in [0, {n}]")
         if parents is not None and len(parents) != n:
             raise ValueError(f"{len(parents)} parents for {n} tokens")
+        _load_torch()
         device = torch.device("cuda", self._dev)
         need = amk_kv_cache_bytes(self.cfg)
         if not kv_cache.is_cuda or kv_cache.device != device:
@@ -645,11 +665,11 @@ class Decoder:
         if n == 0:
             return logits
         lib = load()
-        ws = _workspace(lib.amk_extend_workspace(self.handle, n), device)
+        ws = _workspace(lib.amk_extend_workspace(self.handle, n), self._dev)
         ids = (ctypes.c_int32 * n)(*tokens)
         par = None if parents is None else (ctypes.c_int32 * n)(*parents)
-        _call(device, lib.amk_extend, self.handle, ids, n, pos, par, kv_cache.data_ptr(),
-              logits.data_ptr() if n_logits else None, n_logits, ws.data_ptr(), ws.numel(), _stream(device))
+        _call(self._dev, lib.amk_extend, self.handle, ids, n, pos, par, kv_cache.data_ptr(),
+              logits.data_ptr() if n_logits else None, n_logits, ws.data_ptr(), ws.numel())
         return logits
 
     def score(self, tokens, pos: int, kv_cache, top: int = 0):
