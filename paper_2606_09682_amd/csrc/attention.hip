@@ -236,25 +236,27 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
   top = fmaxf(top, __shfl_xor(top, 32));
-  const float m_new = fmaxf(run.m, top * scale2);
-  const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: p = 2^-inf = 0
-  const float keep = __builtin_amdgcn_exp2f(run.m - base);
-  run.m = m_new;
-  float sum = 0.f;
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      sc[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], scale2, -base));
-      sum += sc[kb][i];
-    }
-  run.l = run.l * keep + sum;
-  if (__any(keep != 1.f)) {
+  // m follows the maximum only where a score exceeds it by 2^8: sums and products lose
+  // nothing by weights of up to 256, and most tiles need not rescale O
+  const float high = top * scale2;
+  if (__any(high > run.m + 8.f)) {
+    const float m = fmaxf(run.m, high);
+    const float keep = __builtin_amdgcn_exp2f(run.m - (m == -INFINITY ? 0.f : m));
+    run.m = m;
+    run.l *= keep;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) run.o[d][i] *= keep;
   }
+  const float base = run.m == -INFINITY ? 0.f : run.m;  // nothing seen yet: p = 2^-inf = 0
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], scale2, -base));
+      run.l += sc[kb][i];
+    }
 
   if constexpr (PARTIAL) {
 #pragma unroll
@@ -347,15 +349,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   if (t0 < t1) from.tile(t0, stages);
   int t = t0, stage = 0;
   for (; t < tf; ++t, stage ^= 1) {
-    wait_loads<0>();
-    __syncthreads();  // tile t is in, and the readers of the other stage are done
+    stage_barrier<0>();  // tile t is in, and the readers of the other stage are done
     AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
     attn_step<HD, WAVES, BN, false>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE,
                                     odd, q, sees, kend, a.scale2, run);
   }
   for (; t < t1; ++t, stage ^= 1) {
-    wait_loads<0>();
-    __syncthreads();
+    stage_barrier<0>();
     AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
     attn_step<HD, WAVES, BN, true>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE, odd,
                                    q, sees, kend, a.scale2, run);
