@@ -321,7 +321,8 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
 
 /* Operands of an attention: bf16 q and out [token][n_heads][head_dim], k and v
  * [row][n_kv_heads][head_dim], each element (t, h, i) at t * token stride +
- * h * head stride + i.  Strides are positive multiples of 8, pointers 16-byte aligned.  One
+ * h * head stride + i.  Strides are positive multiples of 8 (k_token and v_token at most
+ * 2^24), pointers 16-byte aligned.  One
  * layer of the decoder's cache has k_token = head_dim and k_head = max_seq *
  * head_dim.  n_heads is a multiple of n_kv_heads; query head h reads KV head
  * h / (n_heads / n_kv_heads).  head_dim is 64 or 128; scale (positive,

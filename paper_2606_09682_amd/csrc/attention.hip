@@ -142,38 +142,58 @@ __device__ __forceinline__ int v_swizzle(int row) {
   return HD == 128 ? (row & 3) << 2 : (row & 2) << 1;
 }
 
-// Where a workgroup's tiles of K and V come from: this lane's chunk of their first rows.
+// Where a workgroup's tiles of K and V come from: the KV head's rows, and the bytes from a
+// tile's first row to this lane's chunks.
 template <int HD, int WAVES, int BN>
 struct Source {
   static constexpr int CPR = HD / 8;                    // 16-byte chunks per row
-  static constexpr int LOADS = BN * CPR / (64 * WAVES); // loads per lane and tile
+  static constexpr int LOADS = BN * CPR / (64 * WAVES); // loads per lane and tile, of K and of V
   static constexpr int STEP = 64 * WAVES / CPR;         // rows from one load of a lane to its next
-  static_assert(LOADS >= 1 && STEP % 4 == 0, "whole loads, whose V rows share their permutation");
-  const uint16_t *k, *v;  // the KV head's rows
-  int64_t k_token, v_token;
+  static_assert(LOADS >= 1 && BN * CPR % (64 * WAVES) == 0, "whole loads");
+  const unsigned char *k, *v;
+  int64_t k_row, v_row;  // bytes
   int32_t nk;
+  uint32_t ko[LOADS], vo[LOADS];
 
-  // This lane's chunks of tile t: where they are in K and V.
-  __device__ __forceinline__ void chunks(int t, const uint16_t* (&kc)[LOADS], const uint16_t* (&vc)[LOADS]) const {
-    const int row = threadIdx.x / CPR, chunk = threadIdx.x % CPR;
-    const uint16_t *kt = k + (int64_t)(t * BN) * k_token, *vt = v + (int64_t)(t * BN) * v_token;
-    const int left = nk - 1 - t * BN;  // rows past the last key repeat it: in range, and masked
+  static __device__ __forceinline__ uint32_t offset(int row, int64_t stride, int chunk) {
+    return (uint32_t)row * (uint32_t)stride + chunk * 16;  // below 2^32: a row has at most 2^25 bytes
+  }
+  static __device__ __forceinline__ int k_chunk(int row) { return threadIdx.x % CPR ^ k_swizzle<HD>(row); }
+  static __device__ __forceinline__ int v_chunk(int row) { return threadIdx.x % CPR ^ v_swizzle<HD>(row); }
+
+  __device__ __forceinline__ Source(const uint16_t* k_, const uint16_t* v_, int64_t k_token, int64_t v_token, int nk_)
+      : k((const unsigned char*)k_), v((const unsigned char*)v_), k_row(k_token * 2), v_row(v_token * 2), nk(nk_) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int64_t r = min(i * STEP + row, left);
-      kc[i] = kt + r * k_token + (chunk ^ k_swizzle<HD>(row + i * STEP)) * 8;
-      vc[i] = vt + r * v_token + (chunk ^ v_swizzle<HD>(row)) * 8;
+      const int row = i * STEP + threadIdx.x / CPR;
+      ko[i] = offset(row, k_row, k_chunk(row));
+      vo[i] = offset(row, v_row, v_chunk(row));
     }
   }
 
+  // Loads tile t; rows past the last key repeat it: in range, and masked.
   __device__ __forceinline__ void tile(int t, AMK_LDS uint16_t* to) const {
-    const uint16_t *kc[LOADS], *vc[LOADS];
-    chunks(t, kc, vc);
     to += threadIdx.x / 64 * 512;
+    const unsigned char *kt = k + (int64_t)(t * BN) * k_row, *vt = v + (int64_t)(t * BN) * v_row;
+    uint32_t kc[LOADS], vc[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      load_lds16(kc[i], to + i * WAVES * 512);
-      load_lds16(vc[i], to + i * WAVES * 512 + BN * HD);
+      kc[i] = ko[i];
+      vc[i] = vo[i];
+    }
+    const int left = nk - 1 - t * BN;
+    if (left < BN - 1) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = i * STEP + threadIdx.x / CPR;
+        kc[i] = offset(min(row, left), k_row, k_chunk(row));
+        vc[i] = offset(min(row, left), v_row, v_chunk(row));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      load_lds16(kt + kc[i], to + i * WAVES * 512);
+      load_lds16(vt + vc[i], to + i * WAVES * 512 + BN * HD);
     }
   }
 };
@@ -199,16 +219,7 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
                                           int kend, float scale2, Running<HD>& run) {
   constexpr int KB = BN / 32, DB = HD / 32;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-  if (more) {
-    const uint16_t *kc[Source<HD, WAVES, BN>::LOADS], *vc[Source<HD, WAVES, BN>::LOADS];
-    from.chunks(t + 1, kc, vc);
-    AMK_LDS uint16_t* to = next + threadIdx.x / 64 * 512;
-#pragma unroll
-    for (int i = 0; i < Source<HD, WAVES, BN>::LOADS; ++i) {
-      load_lds16(kc[i], to + i * WAVES * 512);
-      load_lds16(vc[i], to + i * WAVES * 512 + BN * HD);
-    }
-  }
+  if (more) from.tile(t + 1, next);
 
   f32x16 sc[KB] = {};
 #pragma unroll
@@ -341,8 +352,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   const int ktiles = (kend + BN - 1) / BN;
   const int t0 = (int)((int64_t)ktiles * split / a.splits), t1 = (int)((int64_t)ktiles * (split + 1) / a.splits);
   const int tf = max(t0, min(t1, kfull / BN));  // tiles that every row sees whole
-  const Source<HD, WAVES, BN> from = {a.k + s.k0 * a.k_token + kvh * a.k_head, a.v + s.k0 * a.v_token + kvh * a.v_head,
-                                      a.k_token, a.v_token, s.nk};
+  const Source<HD, WAVES, BN> from(a.k + s.k0 * a.k_token + kvh * a.k_head, a.v + s.k0 * a.v_token + kvh * a.v_head,
+                                   a.k_token, a.v_token, s.nk);
   if (threadIdx.x == 0) *odd = 0;
   Running<HD> run = {};
   run.m = -INFINITY;
@@ -364,7 +375,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   if (run.odd) {  // rare: add what was set to 0 to the rows that see it
     for (int key = tf * BN; key < min(t1 * BN, kend); ++key) {
       if (!(sees.word(key, kend) & 1)) continue;
-      const uint16_t* vp = from.v + key * a.v_token + 4 * half;
+      const uint16_t* vp = (const uint16_t*)(from.v + key * from.v_row) + 4 * half;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
