@@ -231,6 +231,18 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
       sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
     }
 
+  if constexpr (!PARTIAL) {
+    // K's operands are read four ahead of the products that take them (0x100: LDS reads, 8:
+    // matrix instructions)
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < KB * HD / 16 - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+  }
+
   if constexpr (PARTIAL) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -473,12 +485,17 @@ AttnPlan with_workspace(AttnPlan p, int n_heads, int head_dim, int total_q) {
   return p;
 }
 
-constexpr int kSplitBlocks = 1024;  // workgroups that splits of the keys may add up to
-
 // Workgroups that run at once: each CU has registers for 8 waves.
 int resident(int waves) { return 256 * 8 / waves; }
 
-int waves_for(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+// Waves (32 rows each) of a workgroup.  Eight share a tile of K and V among twice the rows
+// of four, but mask more at a causal diagonal, and `many` says that this pays: heads of 128,
+// us with eight / four waves: one prompt of 8192 tokens 523 / 540, two of 2048 82 / 87, eight
+// of 512 46 / 42; a tree of 64 tokens at 32001 54 / 59.  Heads of 64 gain nothing (a prompt
+// of 8192 330 / 318).
+int waves_for(int64_t rows, int head_dim, bool many) {
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : many && head_dim == 128 ? 8 : 4;
+}
 
 AttnArgs make_args(const amk_attention_t& a, const AttnPlan& p, int total_q, int total_k, void* workspace) {
   AttnArgs r;
@@ -498,7 +515,8 @@ void launch_hd(const AttnArgs& r, const AttnPlan& p, const Which& w, hipStream_t
   const dim3 grid((unsigned)((int64_t)p.tiles * p.splits * r.n_kv));
   if (p.waves == 1) hipLaunchKernelGGL((attn_kernel<HD, 1, 32, Which>), grid, dim3(64), 0, st, r, w);
   else if (p.waves == 2) hipLaunchKernelGGL((attn_kernel<HD, 2, 32, Which>), grid, dim3(128), 0, st, r, w);
-  else hipLaunchKernelGGL((attn_kernel<HD, 4, 64, Which>), grid, dim3(256), 0, st, r, w);
+  else if (p.waves == 4) hipLaunchKernelGGL((attn_kernel<HD, 4, 64, Which>), grid, dim3(256), 0, st, r, w);
+  else if constexpr (HD == 128) hipLaunchKernelGGL((attn_kernel<HD, 8, 64, Which>), grid, dim3(512), 0, st, r, w);
 }
 
 template <typename Which>
@@ -520,14 +538,13 @@ int launch_attn(const AttnArgs& r, const AttnPlan& p, int head_dim, const Which&
 
 // Splits of the keys: as many workgroups as run at once, if every one has `least` keys.
 int splits_for(int64_t blocks, int waves, int64_t keys, int least) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kSplitBlocks, resident(waves)) / blocks,
-                                                     (keys + least - 1) / least));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(resident(waves) / blocks, (keys + least - 1) / least));
 }
 
 AttnPlan prompt_plan(int n_heads, int n_kv_heads, int head_dim, int n_seqs, int total_q, int total_k) {
   AttnPlan p;
   const int64_t rows = (int64_t)total_q * (n_heads / n_kv_heads);
-  p.waves = waves_for(rows);
+  p.waves = waves_for(rows, head_dim, rows / n_seqs >= 8192);
   // whole tiles of the sum, and one that is not whole per sequence
   p.tiles = (int)(rows / (32 * p.waves) + std::min<int64_t>(n_seqs, rows));
   p.splits = splits_for((int64_t)p.tiles * n_kv_heads, p.waves, total_k, 256);
@@ -537,15 +554,18 @@ AttnPlan prompt_plan(int n_heads, int n_kv_heads, int head_dim, int n_seqs, int 
 AttnPlan tree_plan(int n_heads, int n_kv_heads, int head_dim, int n, int pos) {
   AttnPlan p;
   const int64_t rows = (int64_t)n * (n_heads / n_kv_heads);
-  p.waves = waves_for(rows);
+  p.waves = waves_for(rows, head_dim, rows > 128);
   p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  p.splits = splits_for((int64_t)p.tiles * n_kv_heads, p.waves, (int64_t)pos + n, 128);
+  // Up to 320 keys one workgroup is done as soon as two and the join (8 tokens at 300, heads of
+  // 64: 8.4 us against 8.7); beyond, ranges of 128 keys (the same at 600: 11.8 us whole, 8.7).
+  const int64_t keys = (int64_t)pos + n;
+  p.splits = keys <= 320 ? 1 : splits_for((int64_t)p.tiles * n_kv_heads, p.waves, keys, 128);
   return with_workspace(p, n_heads, head_dim, n);
 }
 
 size_t attention_workspace_most(int n_heads, int n_kv_heads, int head_dim) {
-  // a plan with splits has at most kSplitBlocks workgroups of at most 128 rows
-  const size_t rows = (size_t)kSplitBlocks * 128;
+  // a plan with splits has at most resident(waves) workgroups of 32 * waves rows
+  const size_t rows = (size_t)resident(1) * 32;
   return up256(rows * head_dim * sizeof(float)) + rows * sizeof(float2);
 }
 
