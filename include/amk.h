@@ -326,7 +326,8 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
  * layer of the decoder's cache has k_token = head_dim and k_head = max_seq *
  * head_dim.  n_heads is a multiple of n_kv_heads; query head h reads KV head
  * h / (n_heads / n_kv_heads).  head_dim is 64 or 128; scale (positive,
- * finite) multiplies the scores, usually 1 / sqrt(head_dim).
+ * finite) multiplies the scores, usually 1 / sqrt(head_dim).  At most 2^30 rows of k
+ * and 2^30 pairs of a token and a query head.
  * Scores, softmax statistics and the weighted sums are fp32; weights are
  * rounded to bf16 for the product with v.  A row that sees no key, or only keys
  * scoring minus infinity, gets zeros; what a row does not see never reaches it,

@@ -8,6 +8,7 @@ using namespace amk;
 namespace {
 
 constexpr int64_t kMostBlocks = 0x7fffffff;
+constexpr int64_t kMostRows = 1 << 30;  // of an attention: kernels add to row numbers in 32 bits
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
@@ -23,7 +24,7 @@ int check_attention(const amk_attention_t* a, int64_t total_q, int64_t keys) {
     if (!aligned(p, 16)) return AMK_ERR_INVALID_ARGUMENT;
   for (int64_t s : {a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head})
     if (!stride_ok(s)) return AMK_ERR_INVALID_ARGUMENT;
-  if (total_q * a->n_heads > kMostBlocks || a->k_token > 1 << 24 || a->v_token > 1 << 24) return AMK_ERR_UNSUPPORTED;
+  if (total_q * a->n_heads > kMostRows || keys > kMostRows || a->k_token > 1 << 24 || a->v_token > 1 << 24) return AMK_ERR_UNSUPPORTED;
   return AMK_OK;
 }
 

@@ -76,6 +76,7 @@ LINEAR = [  # n, in, out, group
     (1, 64, 1, 64), (1, 256, 64, 32), (2, 96, 33, 32), (15, 320, 65, 64), (16, 576, 1536, 64), (17, 256, 4096, 256),
     (31, 1024, 129, 1024), (33, 2048, 63, 128), (48, 1024, 2500, 128), (64, 688 * 2, 130, 32), (65, 768, 127, 256),
     (129, 4096, 257, 128), (257, 512, 1040, 512), (300, 5632, 300, 64), (512, 320, 515, 64), (1000, 1152, 2051, 128),
+    (2047, 320, 2051, 64), (4090, 576, 4091, 64),  # tiles of 128 and of 256
 ]
 
 
@@ -101,12 +102,12 @@ def test_linear_widths_of_half_steps(env, fmt, width):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "w8a16", "w4a16"])
-@pytest.mark.parametrize("n", [1, 20, 90, 300])
+@pytest.mark.parametrize("n,out", [(1, 130), (20, 130), (90, 130), (300, 130), (64, 14001), (2050, 2050), (4090, 4090)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-def test_linear_strides_and_accumulate(env, fmt, n, dtype):
+def test_linear_strides_and_accumulate(env, fmt, n, out, dtype):
     """Rows apart from each other, what lies between them untouched, and adding to what is there."""
     amk, torch = env
-    width, out, group = 256, 130, 64
+    width, group = 256, 64
     w, s, w64 = matrix(torch, fmt, out, width, group, n)
     store = torch.full((n, width + 24), float("nan"), dtype=torch.bfloat16, device="cuda")
     store[:, 8:8 + width] = randn(torch, 2, n, width).to(torch.bfloat16)
@@ -210,7 +211,8 @@ def test_prompt_attention(env, heads, kv, d, lens_q, lens_k):
         assert torch.equal(amk.prompt_attention(q, k, v), got)
 
 
-@pytest.mark.parametrize("heads,kv,d,nq,nk", [(8, 2, 128, 200, 700), (4, 4, 64, 90, 3000), (4, 1, 64, 513, 513)])
+@pytest.mark.parametrize("heads,kv,d,nq,nk", [(8, 2, 128, 200, 700), (4, 4, 64, 90, 3000), (4, 1, 64, 513, 513),
+                                              (8, 1, 128, 1030, 1100)])
 def test_prompt_attention_longer(env, heads, kv, d, nq, nk):
     """Many key tiles, few row tiles: the keys of a tile may be split over workgroups."""
     amk, torch = env
@@ -218,6 +220,21 @@ def test_prompt_attention_longer(env, heads, kv, d, nq, nk):
     k, v = randn(torch, 2, nk, kv, d).to(torch.bfloat16), randn(torch, 3, nk, kv, d).to(torch.bfloat16)
     got = amk.prompt_attention(q, k, v, scale=0.2)
     close(torch, got, *softmax_rows(torch, q, k, v, prompt_visible(torch, [nq], [nk]), 0.2))
+
+
+def test_prompt_attention_long_contexts_of_several(env):
+    """Sequences of few queries behind long contexts: keys split over workgroups, rows outside every
+    sequence as they were."""
+    amk, torch = env
+    lens_q, lens_k, at = [30, 0, 41], [2999, 7, 2000], 5
+    cu_q, cu_k = offsets(torch, lens_q) + at, offsets(torch, lens_k) + 3
+    q = (randn(torch, 1, 90, 4, 64) * 2).to(torch.bfloat16)
+    k, v = (randn(torch, s, 5100, 2, 64).to(torch.bfloat16) for s in (2, 3))
+    held = randn(torch, 4, 90, 4, 64).to(torch.bfloat16)
+    out = amk.prompt_attention(q, k, v, cu_q, cu_k, out=held.clone())
+    ref, tol = softmax_rows(torch, q[at:76], k[3:5009], v[3:5009], prompt_visible(torch, lens_q, lens_k), 0.125)
+    close(torch, out[at:76], ref, tol)
+    assert torch.equal(out[:at], held[:at]) and torch.equal(out[76:], held[76:])
 
 
 def test_prompt_attention_strides(env):
@@ -238,7 +255,7 @@ def test_prompt_attention_strides(env):
 
 
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
-@pytest.mark.parametrize("heads,kv,d", [(4, 2, 64), (8, 1, 128)])
+@pytest.mark.parametrize("heads,kv,d", [(4, 2, 64), (8, 1, 128), (128, 1, 128)])
 def test_prompt_attention_masked_values_stay_out(env, bad, heads, kv, d):
     """Infinities and NaN in K and V reach only the queries that see them: not those before, nor other
     sequences, nor through rows behind the last."""
@@ -350,10 +367,10 @@ def test_tree_attention_masks(env):
 
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_tree_attention_masked_values_stay_out(env, bad):
-    """A sibling's infinities and NaN do not reach a branch, with keys in one range or in many."""
+    """A sibling's infinities and NaN do not reach a branch, with keys in one range or in many, in small
+    and large workgroups."""
     amk, torch = env
-    for pos in (10, 3000):
-        n, d = 12, 64
+    for pos, n, d in ((10, 12, 64), (3000, 12, 64), (700, 50, 128)):
         q = randn(torch, 1, n, 8, d).to(torch.bfloat16)
         k, v = (randn(torch, s, pos + n, 2, d).to(torch.bfloat16) for s in (2, 3))
         masks = [1 << i | (1 << i % 2) for i in range(n)]  # two branches, of odd and even tokens

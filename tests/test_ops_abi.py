@@ -50,6 +50,7 @@ W8, W4 = {"fmt": amk.AMK_WEIGHTS_W8A16}, {"fmt": amk.AMK_WEIGHTS_W4A16, "width":
     ({"y_type": amk.AMK_F16}, BAD), ({"accumulate": 2}, BAD), ({**W8, "scale": None}, BAD), ({**W8, "scale": P + 2}, BAD),
     ({**W4, "scale": None}, BAD), ({**W4, "scale": P + 1}, BAD), ({**W4, "group": 48}, BAD), ({**W4, "group": 16}, BAD),
     ({**W4, "group": 2048}, BAD), ({**W4, "group": 256}, UNSUPPORTED), ({**W4, "width": 96}, UNSUPPORTED),
+    ({"width": (1 << 22) + 16, "x_stride": (1 << 22) + 16}, UNSUPPORTED), ({"x_stride": (1 << 22) + 8}, UNSUPPORTED),
     ({"n": 0, "x": None, "y": None}, OK), ({"out": 0, "w": None}, OK)])
 def test_linear_refusals(lib, over, status):
     a = {**LINEAR, **over}
@@ -67,7 +68,7 @@ def attention(**over):
 SHARED = [({"q": None}, BAD), ({"k": None}, BAD), ({"v": None}, BAD), ({"out": None}, BAD), ({"q": P + 2}, BAD),
           ({"k": P + 8}, BAD), ({"v": P + 4}, BAD), ({"out": P + 8}, BAD), ({"n_heads": 0}, BAD), ({"n_kv_heads": 0}, BAD),
           ({"n_heads": 5}, UNSUPPORTED), ({"head_dim": 96}, UNSUPPORTED), ({"scale": 0.0}, BAD), ({"scale": -1.0}, BAD),
-          ({"scale": math.inf}, BAD), ({"scale": math.nan}, BAD)]
+          ({"k_token": (1 << 24) + 8}, UNSUPPORTED), ({"v_token": (1 << 24) + 8}, UNSUPPORTED), ({"scale": math.inf}, BAD), ({"scale": math.nan}, BAD)]
 SHARED += [({f"{t}_{s}": v}, BAD) for t in ("q", "k", "v", "out") for s in ("token", "head") for v in (0, -64, 68)]
 
 
@@ -87,7 +88,8 @@ def test_prompt_attention_refusals(lib):
                  (P, P, 1, -1, 5), (P, P, 1, 5, -1), (P + 2, P, 1, 5, 5), (P, P + 1, 1, 5, 5)):
         assert call(*args, None, 0, None) == BAD, args
     assert call(P, P, 0, 5, 5, None, 0, None) == OK and call(P, P, 3, 0, 5, None, 0, None) == OK
-    assert call(P, P, 1, (1 << 31) - 1, 5, P, 1 << 60, None) == UNSUPPORTED
+    assert call(P, P, 1, (1 << 28) + 1, 5, P, 1 << 60, None) == UNSUPPORTED
+    assert call(P, P, 1, 5, (1 << 30) + 1, P, 1 << 60, None) == UNSUPPORTED
     # a workspace that is missing, too small or not aligned, where one is needed
     need = lib.amk_prompt_attention_workspace(4, 2, 64, 1, 65, 20000)
     assert need > 0
@@ -104,6 +106,7 @@ def test_tree_attention_refusals(lib):
     for n, pos, m in ((-1, 0, masks), (65, 0, masks), (1, -1, masks), (1, (1 << 31) - 1, masks), (1, 0, None)):
         assert lib.amk_tree_attention(a, n, pos, m, P, 1 << 40, None) == BAD
     assert lib.amk_tree_attention(a, 0, 0, None, None, 0, None) == OK
+    assert lib.amk_tree_attention(a, 1, 1 << 30, masks, P, 1 << 40, None) == UNSUPPORTED
     need = lib.amk_tree_attention_workspace(4, 2, 64, 8, 5000)
     assert need > 0
     for ws, size in ((None, need), (P, need - 1), (P + 64, need)):
