@@ -53,7 +53,6 @@ struct TokenBlock {
 };
 
 struct LogprobPlan {
-  int32_t chunk;      // vocabulary entries of one workgroup
   int32_t chunks;     // workgroups per row
   size_t workspace;
 };
