@@ -309,7 +309,8 @@ enum { AMK_F32 = 0, AMK_BF16 = 1, AMK_F16 = 2 };
 
 /* y = x W^T (accumulate 0) or y += x W^T (accumulate 1) for n tokens.
  *   x: bf16 [n][in], rows x_stride apart (x and x_stride * 2 bytes 16-byte aligned); in
- *      and x_stride are at most 2^22
+ *      and x_stride are at most 2^22, out at most 2^26; n and out, each rounded up to a
+ *      multiple of 128, have a product of at most 2^36
  *   w, scale: W [out][in] in weight_format, as under amk_linear_t (group_size as in
  *             amk_config_t); in is a multiple of 16, under W4A16 of 32 and of the group
  *   y: fp32 (y_type AMK_F32) or bf16 (AMK_BF16) [n][out], rows y_stride >= out apart
@@ -382,7 +383,7 @@ size_t amk_tree_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t
  *               most probable tokens, the lowest index first among equal logits
  * tokens and logprob, and entropy, may be NULL.  A row that has no softmax (a
  * NaN, plus infinity, or only minus infinities) gets NaN, its top_ids -1.
- * vocab is at most 2^20; n = 0 is a no-op. */
+ * vocab is at most 2^20, n * (vocab / 8192 + 2) below 2^24; n = 0 is a no-op. */
 int amk_token_logprobs(const void* logits, int32_t type, int64_t row_stride, int32_t n, int32_t vocab,
                        const int32_t* tokens, int32_t top, float* logprob, float* entropy, int32_t* top_ids,
                        float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream);

@@ -272,6 +272,7 @@ def amk_schedule_check(cfg: amk_config_t, n_cu: int, tasks, n_counters: int,
 # bare pointers, so types, shapes, devices and strides are checked here.  Small calls
 # take the GPU a few microseconds, so what runs on every call is kept short: a stream
 # is read as its raw handle, and messages are made only for a refusal.
+_SCORE_CHUNK = 2048  # tokens whose logits Decoder.score holds at once: what amk_extend takes through the model at once
 _FORMATS = {"bf16": AMK_WEIGHTS_BF16, "w8a16": AMK_WEIGHTS_W8A16, "w4a16": AMK_WEIGHTS_W4A16}
 _torch = None
 
@@ -309,6 +310,12 @@ def _call(index: int, fn, *args) -> None:
         raise AmkError(status, fn.__name__)
 
 
+def _int32(value: int, what: str) -> None:
+    """Refuses what the library's int32 arguments would silently cut."""
+    if not -1 << 31 <= value < 1 << 31:
+        raise ValueError(f"{what} = {value} does not fit 32 bits")
+
+
 def _device_index(t, what: str) -> int:
     index = t.get_device()
     if index < 0:
@@ -338,6 +345,7 @@ def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, o
         _refuse(w, "w", index, _WEIGHT[fmt], 2)
     n, width = x.shape
     rows, stored = w.shape
+    _int32(n, "n"), _int32(rows, "w's rows"), _int32(group_size, "group_size")
     if n and x.stride(1) != 1:
         raise ValueError("x must have contiguous rows")
     if (stored * 2 if fmt == AMK_WEIGHTS_W4A16 else stored) != width or not w.is_contiguous():
@@ -473,6 +481,7 @@ def token_logprobs(logits, tokens=None, top: int = 0):
     if kind is None or logits.dim() != 2:
         _refuse(logits, "logits", index, tuple(_LOGITS), 2)
     n, vocab = logits.shape
+    _int32(n, "n"), _int32(vocab, "vocab")
     if n and vocab > 1 and logits.stride(1) != 1:
         raise ValueError("logits must have contiguous rows")
     if not 0 <= top <= AMK_TOP_MAX:
@@ -509,6 +518,8 @@ def kv_keep(kv, pos: int, rows) -> None:
         raise ValueError("kv must be a contiguous bf16 tensor [layers, 2, kv heads, max_seq, head_dim]")
     layers, _, heads, cap, d = kv.shape
     n = len(rows)
+    for value in (pos, cap, *rows):
+        _int32(value, "a row")
     _call(index, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n)
 
 
@@ -654,6 +665,10 @@ class Decoder:
             raise ValueError(f"n_logits must be in [0, {n}]")
         if parents is not None and len(parents) != n:
             raise ValueError(f"{len(parents)} parents for {n} tokens")
+        _int32(pos, "pos")
+        for given, what in ((tokens, "a token"), (parents or (), "a parent")):
+            if len(given):
+                _int32(min(given), what), _int32(max(given), what)
         _load_torch()
         device = torch.device("cuda", self._dev)
         need = amk_kv_cache_bytes(self.cfg)
@@ -679,10 +694,16 @@ class Decoder:
         import torch
         if len(tokens) < 2:
             raise ValueError("a text to score has at least two tokens")
-        # the last token's logits predict what follows the text: not needed
-        logits = self.extend(tokens, pos, kv_cache)[:-1]
-        given = torch.tensor(list(tokens[1:]), dtype=torch.int32, device=logits.device)
-        return token_logprobs(logits, given, top)
+        if pos + len(tokens) > self.cfg.max_seq:
+            raise ValueError(f"{len(tokens)} tokens at {pos} exceed the cache's {self.cfg.max_seq} positions")
+        parts = []
+        for at in range(0, len(tokens), _SCORE_CHUNK):
+            piece = tokens[at:at + _SCORE_CHUNK]
+            given = torch.tensor(list(tokens[at + 1:at + 1 + len(piece)]), dtype=torch.int32, device=kv_cache.device)
+            # the last token's logits predict what follows the text: not needed
+            logits = self.extend(piece, pos + at, kv_cache)[:len(given)]
+            parts.append(token_logprobs(logits, given, top))
+        return parts[0] if len(parts) == 1 else tuple(torch.cat(p) for p in zip(*parts))
 
     def keep(self, pos: int, rows, kv_cache) -> None:
         """After extend with a drafted tree at `pos`: make the accepted tokens' rows

@@ -7,7 +7,7 @@ using namespace amk;
 
 namespace {
 
-constexpr int64_t kMostBlocks = 0x7fffffff;
+constexpr int64_t kMostThreads = 0xffffffff;  // of a grid
 constexpr int64_t kMostRows = 1 << 30;  // of an attention: kernels add to row numbers in 32 bits
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
@@ -24,12 +24,14 @@ int check_attention(const amk_attention_t* a, int64_t total_q, int64_t keys) {
     if (!aligned(p, 16)) return AMK_ERR_INVALID_ARGUMENT;
   for (int64_t s : {a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head})
     if (!stride_ok(s)) return AMK_ERR_INVALID_ARGUMENT;
-  if (total_q * a->n_heads > kMostRows || keys > kMostRows || a->k_token > 1 << 24 || a->v_token > 1 << 24) return AMK_ERR_UNSUPPORTED;
+  if (total_q * a->n_heads > kMostRows || keys > kMostRows || a->k_token > 1 << 24 || a->v_token > 1 << 24)
+    return AMK_ERR_UNSUPPORTED;
   return AMK_OK;
 }
 
-bool heads_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
-  return n_heads > 0 && n_kv_heads > 0 && n_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128);
+bool shape_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t total_q, int64_t keys) {
+  return n_heads > 0 && n_kv_heads > 0 && n_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128) &&
+         total_q * n_heads <= kMostRows && keys <= kMostRows;
 }
 
 int check_workspace(const void* p, size_t have, size_t need) {
@@ -56,7 +58,8 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
       !aligned(y, y_type == AMK_F32 ? 4 : 2))
     return AMK_ERR_INVALID_ARGUMENT;
   if (weight_format != AMK_WEIGHTS_BF16 && (!scale || !aligned(scale, w4 ? 2 : 4))) return AMK_ERR_INVALID_ARGUMENT;
-  if (((int64_t)n + 15) / 16 * (((int64_t)out + 15) / 16) > kMostBlocks) return AMK_ERR_UNSUPPORTED;
+  if (out > 1 << 26 || ((int64_t)n + 127) / 128 * (((int64_t)out + 127) / 128) > kMostThreads / 512)
+    return AMK_ERR_UNSUPPORTED;
   LinearArgs a;
   a.x = (const uint16_t*)x; a.x_stride = x_stride; a.n = n; a.in = in; a.out = out; a.w = w; a.scale = scale;
   a.fmt = weight_format; a.group = group; a.y = y; a.y_stride = y_stride; a.y_bf16 = y_type == AMK_BF16;
@@ -66,7 +69,7 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
 
 size_t amk_prompt_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seqs,
                                       int32_t total_q, int32_t total_k) {
-  if (!heads_ok(n_heads, n_kv_heads, head_dim) || n_seqs < 1 || total_q < 1 || total_k < 0) return 0;
+  if (n_seqs < 1 || total_q < 1 || total_k < 0 || !shape_ok(n_heads, n_kv_heads, head_dim, total_q, total_k)) return 0;
   return prompt_plan(n_heads, n_kv_heads, head_dim, n_seqs, total_q, total_k).workspace;
 }
 
@@ -78,14 +81,14 @@ int amk_prompt_attention(const amk_attention_t* a, const int32_t* cu_q, const in
   int st = check_attention(a, total_q, total_k);
   if (st != AMK_OK) return st;
   const AttnPlan p = prompt_plan(a->n_heads, a->n_kv_heads, a->head_dim, n_seqs, total_q, total_k);
-  if ((int64_t)p.tiles * p.splits * a->n_kv_heads > kMostBlocks) return AMK_ERR_UNSUPPORTED;
+  if ((int64_t)p.tiles * p.splits * a->n_kv_heads > kMostThreads / (64 * p.waves)) return AMK_ERR_UNSUPPORTED;
   st = check_workspace(workspace, workspace_bytes, p.workspace);
   if (st != AMK_OK) return st;
   return launch_prompt(*a, p, cu_q, cu_k, n_seqs, total_q, total_k, workspace, stream);
 }
 
 size_t amk_tree_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n, int32_t pos) {
-  if (!heads_ok(n_heads, n_kv_heads, head_dim) || n < 1 || n > AMK_TREE_MAX || pos < 0 || pos > INT32_MAX - n) return 0;
+  if (n < 1 || n > AMK_TREE_MAX || pos < 0 || !shape_ok(n_heads, n_kv_heads, head_dim, n, (int64_t)pos + n)) return 0;
   return tree_plan(n_heads, n_kv_heads, head_dim, n, pos).workspace;
 }
 
@@ -122,7 +125,7 @@ int amk_token_logprobs(const void* logits, int32_t type, int64_t row_stride, int
                         (const void*)top_logprobs})
     if (!aligned(p, 4)) return AMK_ERR_INVALID_ARGUMENT;
   const LogprobPlan p = logprob_plan(type, n, vocab, top);
-  if ((int64_t)n * p.chunks > kMostBlocks) return AMK_ERR_UNSUPPORTED;
+  if ((int64_t)n * p.chunks > kMostThreads / 256) return AMK_ERR_UNSUPPORTED;
   const int st = check_workspace(workspace, workspace_bytes, p.workspace);
   if (st != AMK_OK) return st;
   return launch_logprobs(p, logits, type, row_stride, n, vocab, tokens, top, logprob, entropy, top_ids, top_logprobs,
@@ -136,7 +139,7 @@ int amk_kv_keep(void* kv_cache, int32_t n_layers, int32_t n_kv_heads, int32_t ma
   if (head_dim != 64 && head_dim != 128) return AMK_ERR_UNSUPPORTED;
   if (count == 0) return AMK_OK;
   if (!kv_cache || !rows || !aligned(kv_cache, 16)) return AMK_ERR_INVALID_ARGUMENT;
-  if ((int64_t)n_layers * 2 * n_kv_heads > kMostBlocks) return AMK_ERR_UNSUPPORTED;
+  if ((int64_t)n_layers * 2 * n_kv_heads > kMostThreads / 256) return AMK_ERR_UNSUPPORTED;
   TreeDepths r = {};
   for (int i = 0; i < count; ++i) {
     if (rows[i] < 0 || (i && rows[i] <= rows[i - 1]) || (int64_t)pos + rows[i] >= max_seq) return AMK_ERR_INVALID_ARGUMENT;

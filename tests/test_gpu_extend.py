@@ -269,3 +269,40 @@ def test_extend_on_another_stream_and_in_a_graph(env):
         torch.cuda.synchronize()
         assert torch.equal(a, want) and torch.equal(b, tree) and torch.equal(kv3, rows)
     dec.close()
+
+
+@pytest.mark.parametrize("n", [2048, 2049, 2150])
+def test_score_of_a_long_text_is_taken_in_pieces(env, n):
+    """The pieces are those that extend makes itself, so one extend and one token_logprobs give the same bits."""
+    amk, torch = env
+    cfg, dec, _ = make(amk, "tiny", "bf16", 2304)
+    tokens = [(7 * i * i + 3 * i) % cfg.vocab for i in range(n + 5)]
+    kv, whole = (kv_to_device(empty_cache(cfg, 2304)) for _ in range(2))
+    dec.extend(tokens[:5], 0, kv), dec.extend(tokens[:5], 0, whole)
+    got = dec.score(tokens[5:], 5, kv, top=4)
+    logits = dec.extend(tokens[5:], 5, whole)
+    want = amk.token_logprobs(logits[:-1], torch.tensor(tokens[6:], dtype=torch.int32, device=logits.device), 4)
+    for g, w in zip(got, want):
+        assert g.shape == w.shape and torch.equal(g, w)
+    assert torch.equal(kv, whole)
+    before = kv.clone()
+    with pytest.raises(ValueError):
+        dec.score([1] * 2300, 5, kv)
+    assert torch.equal(kv, before)
+    dec.close()
+
+
+def test_values_past_32_bits_are_refused(env):
+    amk, torch = env
+    cfg, dec, _ = make(amk, "tiny", "bf16", 16)
+    kv = kv_to_device(empty_cache(cfg, 16))
+    for args in (([1, 2], 1 << 32), ([1, (1 << 32) + 2], 0)):
+        with pytest.raises(ValueError):
+            dec.extend(*args, kv)
+    with pytest.raises(ValueError):
+        dec.extend([1, 2], 0, kv, parents=[(1 << 32) - 1, 0])
+    for pos, rows in ((1 << 32, [1]), (0, [1 + (1 << 32)])):
+        with pytest.raises(ValueError):
+            dec.keep(pos, rows, kv)
+    assert not kv.any()
+    dec.close()
