@@ -179,11 +179,7 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
   ws += (kg * G::BR + wr * 32 * G::RB + col) * G::WC * 16;
   const bf16x8 nothing = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   const bf16x8 eight = __builtin_bit_cast(bf16x8, u32x4{kEight, kEight, kEight, kEight});
-  // W4A16: the sums of a group of columns, and of 8 times x there (one for all rows of W)
-  f32x16 part[G::TB][G::RB], off[G::TB];
-#pragma unroll
-  for (int u = 0; u < G::BKW / 32; ++u) {
-    bf16x8 xf[G::TB][2], wf[G::RB][2];
+  auto read_x = [&](int u, bf16x8 (&xf)[G::TB][2]) {
 #pragma unroll
     for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
@@ -192,6 +188,32 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
         xf[tb][s] = *(const AMK_LDS bf16x8*)(xs + 32 * tb * G::XC * 16 + c * 16);
         if (TAIL && kw + 32 * u + 16 * half + 8 * s >= in) xf[tb][s] = nothing;
       }
+  };
+  // W4A16: the sums of a group of columns.  They begin with -8 times those of x, which
+  // are the same for all rows of W.
+  constexpr int US = G::BKW / 32, SPAN = GROUP32 ? 1 : US;  // slices, and those of one group
+  f32x16 part[G::TB][G::RB];
+  bf16x8 xf[W4 ? SPAN : 1][G::TB][2];
+#pragma unroll
+  for (int u = 0; u < US; ++u) {
+    bf16x8 wf[G::RB][2];
+    if constexpr (W4) {
+      if (u % SPAN == 0) {
+#pragma unroll
+        for (int i = 0; i < SPAN; ++i) read_x(u + i, xf[i]);
+#pragma unroll
+        for (int tb = 0; tb < G::TB; ++tb) {
+          f32x16 off = {};
+#pragma unroll
+          for (int i = 0; i < 2 * SPAN; ++i)
+            off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[i / 2][tb][i % 2], eight, off, 0, 0, 0);
+#pragma unroll
+          for (int rb = 0; rb < G::RB; ++rb) part[tb][rb] = off;
+        }
+      }
+    } else {
+      read_x(u, xf[0]);
+    }
 #pragma unroll
     for (int rb = 0; rb < G::RB; ++rb) {
       const AMK_LDS unsigned char* wrow = ws + 32 * rb * G::WC * 16;
@@ -214,32 +236,23 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
           if (kw + 32 * u + 16 * half + 8 * s >= in) wf[rb][s] = nothing;
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const bool first = W4 && s == 0 && (GROUP32 || u == 0);
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int tb = 0; tb < G::TB; ++tb) {
+      for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
         for (int rb = 0; rb < G::RB; ++rb) {
           f32x16& sum = W4 ? part[tb][rb] : acc[tb][rb];
-          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], wf[rb][s], first ? f32x16{} : sum, 0, 0, 0);
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[W4 ? u % SPAN : 0][tb][s], wf[rb][s], sum, 0, 0, 0);
         }
-        if constexpr (W4) {
-          f32x16& sum = G::RB == 1 ? part[tb][0] : off[tb];
-          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], eight, first && G::RB > 1 ? f32x16{} : sum, 0, 0, 0);
-        }
-      }
-    }
     if constexpr (W4) {
-      if (GROUP32 || u + 1 == G::BKW / 32) {
+      if (u % SPAN == SPAN - 1) {
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
           for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              acc[tb][rb][e] = __builtin_fmaf(scale[rb][GROUP32 ? u : 0],
-                                              G::RB == 1 ? part[tb][rb][e] : part[tb][rb][e] + off[tb][e],
-                                              acc[tb][rb][e]);
+              acc[tb][rb][e] = __builtin_fmaf(scale[rb][u / SPAN], part[tb][rb][e], acc[tb][rb][e]);
       }
     }
   }
@@ -323,7 +336,8 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
     slot = slot == AHEAD ? 0 : slot + 1;
   };
   while (k0 + G::COLS <= a.in) take(std::false_type());
-  if (k0 < a.in) take(std::true_type());
+  if constexpr (!(W4 && !GROUP32 && G::KG == 1))  // else the columns are whole groups, and these whole stages
+    if (k0 < a.in) take(std::true_type());
 
   if constexpr (G::KG == 1) {
     by_output(a, [&](auto bf16, auto add) {
@@ -375,10 +389,13 @@ template <int FMT, typename G>
 int launch_tile(const LinearArgs& a, hipStream_t st) {
   const int tt = (a.n + G::BT - 1) / G::BT, rt = (a.out + G::BR - 1) / G::BR;
   const dim3 grid((unsigned)(((int64_t)tt * rt + 7) / 8 * 8));
-  if (FMT == AMK_WEIGHTS_W4A16 && a.group == 32)
-    hipLaunchKernelGGL((linear_kernel<FMT, G, FMT == AMK_WEIGHTS_W4A16>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
-  else
-    hipLaunchKernelGGL((linear_kernel<FMT, G, false>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
+  if constexpr (FMT == AMK_WEIGHTS_W4A16 && G::BKW <= 64) {
+    if (a.group == 32) {
+      hipLaunchKernelGGL((linear_kernel<FMT, G, true>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
+      return hipGetLastError() == hipSuccess ? AMK_OK : AMK_ERR_DEVICE;
+    }
+  }
+  hipLaunchKernelGGL((linear_kernel<FMT, G, false>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
   return hipGetLastError() == hipSuccess ? AMK_OK : AMK_ERR_DEVICE;
 }
 
@@ -403,6 +420,13 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
   // the time of whole rounds of tiles: a 256 x 256 tile to a CU, or two of 128 x 128, which
   // take about 0.6 of its time together
   const int64_t large = (t256 + 255) / 256 * 10, medium = (t128 + 511) / 512 * 6;
+  if constexpr (W4) {
+    // where groups allow it, stages of 128 columns: half as many sums to scale, 2048 tokens
+    // 4096 -> 14336 309 us (345 with stages of 64)
+    if (a.group >= 128)
+      return large <= medium ? launch_tile<FMT, Tile<FMT, 2, 2, 2, 4, 1, 128>>(a, st)
+                             : launch_tile<FMT, Tile<FMT, 2, 2, 2, 2, 1, 128>>(a, st);
+  }
   if (large <= medium) return launch_tile<FMT, Tile<FMT, W4 ? 2 : 4, 2, 2, 4, 1, 64>>(a, st);
   return launch_tile<FMT, Tile<FMT, 2, 2, 2, 2, 1, 64>>(a, st);
 }

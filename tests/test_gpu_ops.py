@@ -91,6 +91,16 @@ def test_linear(env, fmt, n, width, out, group):
         check_linear(torch, y, x, w64)
 
 
+@pytest.mark.parametrize("n,width,out,group", [
+    (2050, 384, 2060, 128), (2050, 512, 8200, 256), (2048, 1024, 8192, 1024), (2050, 128, 8200, 128),
+    (2050, 96, 8200, 32), (2050, 192, 8200, 64), (1030, 160, 4100, 32)])
+def test_linear_groups_in_large_tiles(env, n, width, out, group):
+    amk, torch = env
+    w, s, w64 = matrix(torch, "w4a16", out, width, group, n)
+    x = randn(torch, 1, n, width).to(torch.bfloat16)
+    check_linear(torch, amk.linear(x, w, s, "w4a16", group), x, w64)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "w8a16"])
 @pytest.mark.parametrize("width", [16, 48, 80, 2768])
 def test_linear_widths_of_half_steps(env, fmt, width):
