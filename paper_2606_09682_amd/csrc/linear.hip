@@ -161,8 +161,9 @@ struct Source {
 };
 
 // The products of this wave's share of the stage of columns k0 .., while the one that
-// takes the place of the stage before (if more follow) is loaded into `next`.  xs, ws and next do not overlap: without that
-// promise every read would wait for the loads.  TAIL: columns past the last count as 0.
+// takes the place of the stage before (if more follow) is loaded into `next`.  xs, ws and
+// next do not overlap: without that promise every read would wait for the loads.  TAIL:
+// columns past the last count as 0.
 template <int FMT, typename G, bool TAIL, bool GROUP32>
 __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k0, bool more,
                                             const AMK_LDS unsigned char* __restrict__ xs,
@@ -406,15 +407,26 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
   const int64_t t64 = (int64_t)((a.n + 63) / 64) * ((a.out + 63) / 64);
   const int64_t t128 = (int64_t)((a.n + 127) / 128) * ((a.out + 127) / 128);
   const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
-  // few tokens, padded to 16 only, a ring of three: 16 tokens bf16 4096 -> 4096 8.3 us, with two 11.5
-  if (a.n <= 16) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32, W4 ? 2 : 3, 16>>(a, st);
+  // Few tokens, or too few tiles of 128 x 128: small tiles, their columns over 4 to 16 waves.
+  // Stages of bf16 and int8 come in rings of three (30 tokens 14336 -> 4096 bf16 41 us, with two
+  // 54); those of int4 wait for their scales (see linear_kernel), and where the tiles leave CUs
+  // idle, 16 waves a tile hide some of that (30 tokens 14336 -> 4096 23.2 us, with 8 26.5).
+  if (a.n <= 16) {  // x is padded to 16 only: 16 tokens bf16 4096 -> 4096 8.3 us, with 32 9.5
+    if constexpr (W4)
+      if (t32 < 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 16, 64, 2, 16>>(a, st);
+    return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32, W4 ? 2 : 3, 16>>(a, st);
+  }
   if (t128 < 256) {
-    // Not enough for large tiles: whole rounds of 32 x 32, two to a CU, or of 64 x 64, which
-    // load the same bytes in a round and half as many a product.  128 tokens int8 4096 -> 4096
-    // 14.0 us in one round of 32 x 32 (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336
-    // 34.3 us in one round of 64 x 64 (42.8 in two of 32 x 32).
-    if (a.n <= 32 || (t32 + 511) / 512 <= (t64 + 255) / 256)
-      return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+    // Whole rounds of 32 x 32, two to a CU, or of 64 x 64, which load the same bytes in a round
+    // and half as many a product.  128 tokens int8 4096 -> 4096 13.0 us in one round of 32 x 32
+    // (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336 34.3 us in one round of 64 x 64 (42.8
+    // in two of 32 x 32).  Where every CU has a tile of 32 x 32, 4 waves each are enough (32 tokens
+    // int8 4096 -> 8192 10.4 us, with 8 14.0), and bf16, whose stages are the largest, needs room
+    // for two tiles more than a third stage (32 tokens 4096 -> 14336 27.1 us, with three 28.8).
+    if (a.n <= 32 || (t32 + 511) / 512 <= (t64 + 255) / 256) {
+      if (t32 < 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, W4 ? 16 : 8, W4 ? 64 : 32, W4 ? 2 : 3>>(a, st);
+      return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 4, 64, FMT == AMK_WEIGHTS_W8A16 ? 3 : 2>>(a, st);
+    }
     return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
   }
   // the time of whole rounds of tiles: a 256 x 256 tile to a CU, or two of 128 x 128, which
