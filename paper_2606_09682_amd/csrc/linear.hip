@@ -417,17 +417,21 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
     return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32, W4 ? 2 : 3, 16>>(a, st);
   }
   if (t128 < 256) {
-    // Whole rounds of 32 x 32, two to a CU, or of 64 x 64, which load the same bytes in a round
-    // and half as many a product.  128 tokens int8 4096 -> 4096 13.0 us in one round of 32 x 32
-    // (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336 34.3 us in one round of 64 x 64 (42.8
-    // in two of 32 x 32).  Where every CU has a tile of 32 x 32, 4 waves each are enough (32 tokens
-    // int8 4096 -> 8192 10.4 us, with 8 14.0), and bf16, whose stages are the largest, needs room
-    // for two tiles more than a third stage (32 tokens 4096 -> 14336 27.1 us, with three 28.8).
-    if (a.n <= 32 || (t32 + 511) / 512 <= (t64 + 255) / 256) {
+    // One round of 32 x 32, two to a CU, where that takes them all, otherwise 64 x 64, which load
+    // the same bytes in a round and half as many a product: 128 tokens int8 4096 -> 4096 13.0 us
+    // in one round of 32 x 32 (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336 34.3 us in one
+    // round of 64 x 64 (42.8 in two of 32 x 32).  Where every CU has a tile of 32 x 32, 4 waves
+    // each are enough (32 tokens int8 4096 -> 8192 10.4 us, with 8 14.0), and bf16, whose stages
+    // are the largest, needs room for two tiles more than a third stage (32 tokens 4096 -> 14336
+    // 27.1 us, with three 28.8).
+    if (a.n <= 32 || t32 <= 512) {
       if (t32 < 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, W4 ? 16 : 8, W4 ? 64 : 32, W4 ? 2 : 3>>(a, st);
       return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 4, 64, FMT == AMK_WEIGHTS_W8A16 ? 3 : 2>>(a, st);
     }
-    return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+    // 64 x 64: 8 waves on one tile a CU, or 4 waves each on two.  300 tokens bf16 4096 -> 4096, 320
+    // tiles, 26.4 us two to a CU (43.2 one); 200 tokens 14336 -> 4096, 256 tiles, 78 us one (104 two).
+    if (t64 <= 256) return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 8, W4 ? 64 : 32>>(a, st);
+    return launch_tile<FMT, Tile<FMT, 2, 2, 1, 1, 4, W4 ? 64 : 32>>(a, st);
   }
   // the time of whole rounds of tiles: a 256 x 256 tile to a CU, or two of 128 x 128, which
   // take about 0.6 of its time together

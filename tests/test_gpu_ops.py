@@ -91,6 +91,17 @@ def test_linear(env, fmt, n, width, out, group):
         check_linear(torch, y, x, w64)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "w8a16", "w4a16"])
+@pytest.mark.parametrize("n,width,out,group", [(31, 1152, 8190, 128), (100, 1056, 4096, 32), (97, 5504, 14330, 64),
+                                               (200, 1088, 4090, 64), (300, 416, 4090, 32), (511, 5504, 4099, 128)])
+def test_linear_small_tiles(env, fmt, n, width, out, group):
+    """More tiles of 32 than CUs, one round of tiles of 64 and two to a CU, columns that end inside a stage."""
+    amk, torch = env
+    w, s, w64 = matrix(torch, fmt, out, width, group, n)
+    x = randn(torch, 1, n, width).to(torch.bfloat16)
+    check_linear(torch, amk.linear(x, w, s, fmt, group), x, w64)
+
+
 @pytest.mark.parametrize("n,width,out,group", [
     (2050, 384, 2060, 128), (2050, 512, 8200, 256), (2048, 1024, 8192, 1024), (2050, 128, 8200, 128),
     (2050, 96, 8200, 32), (2050, 192, 8200, 64), (1030, 160, 4100, 32)])
