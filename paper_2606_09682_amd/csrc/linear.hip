@@ -409,23 +409,23 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
   const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
   // Few tokens, or too few tiles of 128 x 128: small tiles, their columns over 4 to 16 waves.
   // Stages of bf16 and int8 come in rings of three (30 tokens 14336 -> 4096 bf16 41 us, with two
-  // 54); those of int4 wait for their scales (see linear_kernel), and where the tiles leave CUs
-  // idle, 16 waves a tile hide some of that (30 tokens 14336 -> 4096 23.2 us, with 8 26.5).
+  // 54); those of int4 wait for their scales (see linear_kernel), and where a CU takes one
+  // tile, 16 waves on it hide some of that (30 tokens 14336 -> 4096 23.2 us, with 8 26.5).
   if (a.n <= 16) {  // x is padded to 16 only: 16 tokens bf16 4096 -> 4096 8.3 us, with 32 9.5
     if constexpr (W4)
-      if (t32 < 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 16, 64, 2, 16>>(a, st);
+      if (t32 <= 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 16, 64, 2, 16>>(a, st);
     return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 8, W4 ? 64 : 32, W4 ? 2 : 3, 16>>(a, st);
   }
   if (t128 < 256) {
     // One round of 32 x 32, two to a CU, where that takes them all, otherwise 64 x 64, which load
     // the same bytes in a round and half as many a product: 128 tokens int8 4096 -> 4096 13.0 us
     // in one round of 32 x 32 (20.5 in one of 64 x 64); 64 tokens bf16 4096 -> 14336 34.3 us in one
-    // round of 64 x 64 (42.8 in two of 32 x 32).  Where every CU has a tile of 32 x 32, 4 waves
-    // each are enough (32 tokens int8 4096 -> 8192 10.4 us, with 8 14.0), and bf16, whose stages
-    // are the largest, needs room for two tiles more than a third stage (32 tokens 4096 -> 14336
-    // 27.1 us, with three 28.8).
+    // round of 64 x 64 (42.8 in two of 32 x 32).  Where CUs take two tiles of 32 x 32, 4 waves each
+    // do (32 tokens int8 4096 -> 14336 13.8 us, with 8 14.9; one tile a CU, 4096 -> 8192, 10.0 and
+    // 9.4), and bf16, whose stages are the largest, needs room for two tiles more than a third
+    // stage (32 tokens 4096 -> 14336 27.1 us, with three 28.8).
     if (a.n <= 32 || t32 <= 512) {
-      if (t32 < 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, W4 ? 16 : 8, W4 ? 64 : 32, W4 ? 2 : 3>>(a, st);
+      if (t32 <= 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, W4 ? 16 : 8, W4 ? 64 : 32, W4 ? 2 : 3>>(a, st);
       return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 4, 64, FMT == AMK_WEIGHTS_W8A16 ? 3 : 2>>(a, st);
     }
     // 64 x 64: 8 waves on one tile a CU, or 4 waves each on two.  300 tokens bf16 4096 -> 4096, 320
