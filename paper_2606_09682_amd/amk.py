@@ -518,8 +518,9 @@ def kv_keep(kv, pos: int, rows) -> None:
         raise ValueError("kv must be a contiguous bf16 tensor [layers, 2, kv heads, max_seq, head_dim]")
     layers, _, heads, cap, d = kv.shape
     n = len(rows)
-    for value in (pos, cap, *rows):
-        _int32(value, "a row")
+    _int32(pos, "pos"), _int32(cap, "max_seq")
+    if n:
+        _int32(min(rows), "a row"), _int32(max(rows), "a row")
     _call(index, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n)
 
 

@@ -30,6 +30,15 @@
 // then 0, but 0 * V is NaN where V holds an infinity or NaN, so in tiles that
 // some row sees only in part such values of V are set to 0 before the product;
 // if there were any, they are added at the end to the rows that see their key.
+//
+// What bounds it.  The two waves of a SIMD take turns at products and softmax: at a
+// prompt of 8192 tokens, 32 query and 8 KV heads of 128, the matrix cores are busy 51%
+// of the time and no LDS read meets another's bank: 535 us, 1030 TFLOP/s (a large bf16
+// product reaches 1380).  Heads of 64 do half the products for the same softmax: six
+// packed sequences of 4092 tokens, 32 and 4 heads, 50 us, 610 TFLOP/s.  64 drafted tokens
+// at position 32001, 32 and 8 heads of 128, take 46 us and 9 more to join 32 splits (33
+// MB of partial sums): 2.4 TB/s, where both the keys and the products have a floor of 24.
+// Eight tokens at 300, 9 and 3 heads of 64, take 8.5 us, ten tiles one after another.
 #include <algorithm>
 #include <cmath>
 

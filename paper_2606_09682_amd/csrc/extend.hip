@@ -1,6 +1,7 @@
 // Elementwise kernels of amk_extend, and the rows of a KV cache moved together.
-// All of them read and write each byte once and are bound by HBM at thousands
-// of tokens and by their launch at few.
+// All of them read and write each byte once (the norm reads its row twice, the
+// second time from L2) and are bound by HBM at thousands of tokens and by their launch at
+// few: keeping 7 rows in 512 planes of 128-wide heads takes 2.8 us for 1.8 MB.
 #include "ops.h"
 #include "ops_device.h"
 

@@ -5,8 +5,8 @@
 // lane's results lie in one row of W, so one scale serves all of them: W8A16
 // multiplies the finished sums, W4A16 the sums over a group of columns.
 //
-// x and the raw bytes of W go straight to LDS (16 bytes a lane), two stages, a
-// stage's loads under the other's products.  Codes become bf16 (exactly) in
+// x and the raw bytes of W go straight to LDS (16 bytes a lane), two or three stages,
+// the loads of one or two under the products of another.  Codes become bf16 (exactly) in
 // registers, after the read from LDS: a quantised W takes its smaller share of
 // HBM, L2 and LDS alike, and the conversions of one wave run beside the products
 // of another.  Rows lie without padding, their 16-byte chunks permuted by the row
@@ -21,6 +21,13 @@
 // through LDS at the end.  Long prompts need large tiles, few reads of LDS a product
 // (KG 1); few tokens need the weights streamed by every CU, so small tiles and many
 // waves on their columns.
+//
+// What bounds it.  2048 tokens 4096 -> 14336: matrix cores (busy 55% of the time; 448
+// tiles of 256 x 256 are 1.75 rounds of the CUs), bf16 232 us, 1035 TFLOP/s (the library's
+// product 208, a large square one 1380); int8 240; int4, which also converts and scales
+// sums, 305.  32 tokens 4096 -> 14336: bf16 27 us (4.4 TB/s), int8 13.7, int4 13.9: with
+// the smaller formats the copies of x that every tile reads from L2, 117 MB, weigh more
+// than the weights.  5 tokens int8 576 -> 1536 take 3.6 us, hardly more than a launch.
 #include <type_traits>
 
 #include "ops.h"
