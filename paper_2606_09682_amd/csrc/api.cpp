@@ -723,11 +723,12 @@ int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, co
   const int H = s.H, I = s.I, qd = s.nq * s.hd, kd = s.nkv * s.hd, qkvd = qd + 2 * kd;
   const int64_t plane = (int64_t)s.max_seq * s.hd;
 
-  auto linear = [&](const uint16_t* in, int width, int rows, const void* w, const void* sc, int fmt, int out, float* y,
+  auto linear = [&](const uint16_t* in, int width, int rows, std::initializer_list<amk::LinearPart> parts, int fmt,
                     int64_t y_stride, int accumulate) {
-    amk::LinearArgs a;
-    a.x = in; a.x_stride = width; a.n = rows; a.in = width; a.out = out; a.w = w; a.scale = sc; a.fmt = fmt;
-    a.group = s.qgroup; a.y = y; a.y_stride = y_stride; a.y_bf16 = 0; a.accumulate = accumulate;
+    amk::LinearArgs a = {};
+    a.x = in; a.x_stride = width; a.n = rows; a.in = width; a.fmt = fmt; a.group = s.qgroup;
+    for (const amk::LinearPart& p : parts) a.part[a.parts++] = p;
+    a.y_stride = y_stride; a.y_bf16 = 0; a.accumulate = accumulate;
     return amk::launch_linear(a, stream);
   };
 
@@ -751,9 +752,9 @@ int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, co
       uint16_t* k = (uint16_t*)kv_cache + (int64_t)l * 2 * s.nkv * plane;
       uint16_t* v = k + s.nkv * plane;
       if (st == AMK_OK) st = amk::launch_rmsnorm(x, w.attn_norm, c, H, s.eps, hb, stream);
-      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_Q], w.s[amk::W_Q], s.fmt, qd, qkv, qkvd, 0);
-      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_K], w.s[amk::W_K], s.fmt, kd, qkv + qd, qkvd, 0);
-      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_V], w.s[amk::W_V], s.fmt, kd, qkv + qd + kd, qkvd, 0);
+      if (st == AMK_OK)
+        st = linear(hb, H, c, {{w.w[amk::W_Q], w.s[amk::W_Q], qkv, qd}, {w.w[amk::W_K], w.s[amk::W_K], qkv + qd, kd},
+                               {w.w[amk::W_V], w.s[amk::W_V], qkv + qd + kd, kd}}, s.fmt, qkvd, 0);
       if (st == AMK_OK)
         st = amk::launch_rope_append(qkv, h->dm.rope, c, at, parents ? &depths : nullptr, s.nq, s.nkv, s.hd, s.max_seq,
                                      q, k, v, stream);
@@ -766,19 +767,19 @@ int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, co
           st = amk::launch_prompt(a, amk::prompt_plan(s.nq, s.nkv, s.hd, 1, c, at + c), nullptr, nullptr, 1, c, at + c,
                                   attn_ws, stream);
       }
-      if (st == AMK_OK) st = linear(o, qd, c, w.w[amk::W_O], w.s[amk::W_O], s.fmt, H, x, H, 1);
+      if (st == AMK_OK) st = linear(o, qd, c, {{w.w[amk::W_O], w.s[amk::W_O], x, H}}, s.fmt, H, 1);
       if (st == AMK_OK) st = amk::launch_rmsnorm(x, w.mlp_norm, c, H, s.eps, hb, stream);
-      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_G], w.s[amk::W_G], s.fmt, I, gate, I, 0);
-      if (st == AMK_OK) st = linear(hb, H, c, w.w[amk::W_U], w.s[amk::W_U], s.fmt, I, up, I, 0);
+      if (st == AMK_OK)
+        st = linear(hb, H, c, {{w.w[amk::W_G], w.s[amk::W_G], gate, I}, {w.w[amk::W_U], w.s[amk::W_U], up, I}}, s.fmt, I, 0);
       if (st == AMK_OK) st = amk::launch_silu_mul(gate, up, (int64_t)c * I, act, stream);
-      if (st == AMK_OK) st = linear(act, I, c, w.w[amk::W_D], w.s[amk::W_D], s.fmt, H, x, H, 1);
+      if (st == AMK_OK) st = linear(act, I, c, {{w.w[amk::W_D], w.s[amk::W_D], x, H}}, s.fmt, H, 1);
     }
     // logits of this chunk's tokens among the last n_logits
     const int first = std::max(c0, n - n_logits), m = c0 + c - first;
     if (st == AMK_OK && m > 0) {
       st = amk::launch_rmsnorm(x + (size_t)(first - c0) * H, h->dm.final_norm, m, H, s.eps, hb, stream);
       if (st == AMK_OK)
-        st = linear(hb, H, m, h->dm.lm_w, h->dm.lm_s, h->dm.lm_fmt, s.V, logits + (int64_t)(first - (n - n_logits)) * s.V,
+        st = linear(hb, H, m, {{h->dm.lm_w, h->dm.lm_s, logits + (int64_t)(first - (n - n_logits)) * s.V, s.V}}, h->dm.lm_fmt,
                     s.V, 0);
     }
     if (st != AMK_OK) return st;

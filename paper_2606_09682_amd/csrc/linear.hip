@@ -20,7 +20,8 @@
 // groups of waves that share the tile and take a share of the columns each, joined
 // through LDS at the end.  Long prompts need large tiles, few reads of LDS a product
 // (KG 1); few tokens need the weights streamed by every CU, so small tiles and many
-// waves on their columns.
+// waves on their columns.  A launch may take up to three matrices that x is multiplied
+// with (Q, K and V; gate and up), whose tiles fill the CUs together.
 //
 // What bounds it.  2048 tokens 4096 -> 14336: matrix cores (busy 55% of the time; 448
 // tiles of 256 x 256 are 1.75 rounds of the CUs), bf16 232 us, 1035 TFLOP/s (the library's
@@ -120,9 +121,9 @@ struct Source {
   const unsigned char *x, *w;
   uint32_t xo[G::XLOADS], wo[G::WLOADS];
 
-  __device__ __forceinline__ Source(const LinearArgs& a, int t0, int r0) {
+  __device__ __forceinline__ Source(const LinearArgs& a, const LinearPart& p, int t0, int r0) {
     x = (const unsigned char*)(a.x + (int64_t)t0 * a.x_stride);
-    w = (const unsigned char*)a.w + (int64_t)r0 * (a.in / 8) * G::EIGHT;
+    w = (const unsigned char*)p.w + (int64_t)r0 * (a.in / 8) * G::EIGHT;
 #pragma unroll
     for (int i = 0; i < G::XLOADS; ++i) {
       const Lane<G> l = Lane<G>::x(i);
@@ -131,7 +132,7 @@ struct Source {
 #pragma unroll
     for (int i = 0; i < G::WLOADS; ++i) {
       const Lane<G> l = Lane<G>::w(i);
-      wo[i] = (uint32_t)min(l.row, a.out - 1 - r0) * (uint32_t)(a.in / 8) * G::EIGHT + l.k / 8 * G::EIGHT;
+      wo[i] = (uint32_t)min(l.row, p.out - 1 - r0) * (uint32_t)(a.in / 8) * G::EIGHT + l.k / 8 * G::EIGHT;
     }
   }
 
@@ -267,12 +268,12 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
 }
 
 template <bool BF16, bool ADD>
-__device__ __forceinline__ void put(const LinearArgs& a, int64_t at, float y) {
+__device__ __forceinline__ void put(void* to, int64_t at, float y) {
   if (BF16) {
-    uint16_t* p = (uint16_t*)a.y + at;
+    uint16_t* p = (uint16_t*)to + at;
     *p = f32_to_bf16(ADD ? bf16_to_f32(*p) + y : y);
   } else {
-    float* p = (float*)a.y + at;
+    float* p = (float*)to + at;
     *p = ADD ? *p + y : y;
   }
 }
@@ -284,7 +285,9 @@ __device__ __forceinline__ void by_output(const LinearArgs& a, F f) {
   else a.accumulate ? f(std::false_type(), std::true_type()) : f(std::false_type(), std::false_type());
 }
 
-template <int FMT, typename G, bool GROUP32>
+// MANY: more than one matrix.  One alone is read straight from the arguments, since choosing
+// costs its loads their early start (32 tokens int4 4096 -> 14336 14.2 us, chosen 14.7).
+template <int FMT, typename G, bool GROUP32, bool MANY>
 __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs a, int token_tiles, int row_tiles) {
   __shared__ __align__(16) unsigned char lds[G::LDS];
   AMK_LDS unsigned char* mem = (AMK_LDS unsigned char*)lds;
@@ -295,16 +298,28 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
   const int tiles = token_tiles * row_tiles, each = (tiles + 7) / 8;
   const int tile = (int)(blockIdx.x % 8) * each + (int)(blockIdx.x / 8);
   if ((int)(blockIdx.x / 8) >= each || tile >= tiles) return;
-  const int t0 = tile % token_tiles * G::BT, r0 = tile / token_tiles * G::BR;
+  // the row tiles of each matrix follow those of the one before
+  int row_tile = tile / token_tiles;
+  LinearPart part = a.part[0];
+#pragma unroll
+  for (int i = 1; i < (MANY ? 3 : 1); ++i) {
+    const int before = (part.out + G::BR - 1) / G::BR;
+    if (i < a.parts && row_tile >= before) {
+      row_tile -= before;
+      part = a.part[i];
+    }
+  }
+  const int t0 = tile % token_tiles * G::BT, r0 = row_tile * G::BR;
 
   // under W4A16: this lane's rows of the scales, and the scales of its wave's next slice
   constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
   const int groups = W4 ? a.in / a.group : 0, shift = W4 ? __builtin_ctz(a.group) : 0;
   const uint16_t* srow[G::RB];
-  uint16_t ahead[G::RB][2];
+  uint32_t ahead[G::RB][2];
 #pragma unroll
   for (int rb = 0; rb < G::RB; ++rb)
-    srow[rb] = (const uint16_t*)a.scale + (int64_t)min(r0 + (wr * G::RB + rb) * 32 + col, a.out - 1) * groups;
+    srow[rb] = (const uint16_t*)part.scale +
+               (int64_t)min(r0 + (wr * G::RB + rb) * 32 + col, part.out - 1) * groups;
   auto fetch = [&](int k0) {
     if constexpr (W4)
 #pragma unroll
@@ -315,7 +330,7 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
   };
 
   f32x16 acc[G::TB][G::RB] = {};
-  const Source<G> from(a, t0, r0);
+  const Source<G> from(a, part, t0, r0);
   constexpr int AHEAD = G::STAGES - 1;  // stages under way behind the one in use
   constexpr int LOADS = G::XLOADS + G::WLOADS;
   static_assert(!W4 || AHEAD == 1, "scales are fetched one stage ahead: waiting for them is waiting for all");
@@ -334,7 +349,11 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
 #pragma unroll
       for (int rb = 0; rb < G::RB; ++rb)
 #pragma unroll
-        for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u) scale[rb][u] = half_to_f32(ahead[rb][u]) * kStep;
+        for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u) {
+          // with MANY the compiler converts a scale, and so waits for it, where it was loaded
+          if constexpr (MANY) asm volatile("" : "+v"(ahead[rb][u]));
+          scale[rb][u] = half_to_f32((uint16_t)ahead[rb][u]) * kStep;
+        }
     }
     fetch(k0 + G::COLS);
     AMK_LDS unsigned char *cur = mem + slot * G::STAGE, *next = mem + (slot ? slot - 1 : AHEAD) * G::STAGE;
@@ -352,14 +371,14 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
 #pragma unroll
       for (int rb = 0; rb < G::RB; ++rb) {
         const int r = r0 + (wr * G::RB + rb) * 32 + col;
-        if (r >= a.out) continue;
-        const float sc = FMT == AMK_WEIGHTS_W8A16 ? ((const float*)a.scale)[r] : 1.f;
+        if (r >= part.out) continue;
+        const float sc = FMT == AMK_WEIGHTS_W8A16 ? ((const float*)part.scale)[r] : 1.f;
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int t = t0 + (wt * G::TB + tb) * 32 + 8 * (e / 4) + 4 * half + e % 4;
-            if (t < a.n) put<decltype(bf16)::value, decltype(add)::value>(a, t * a.y_stride + r, acc[tb][rb][e] * sc);
+            if (t < a.n) put<decltype(bf16)::value, decltype(add)::value>(part.y, t * a.y_stride + r, acc[tb][rb][e] * sc);
           }
       }
     });
@@ -382,38 +401,45 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
         const int o = n * G::THREADS + threadIdx.x;
         const int l = o % 64, e = o / 64 % 16, rb = o / 1024 % G::RB, tb = o / 1024 / G::RB;
         const int t = t0 + tb * 32 + 8 * (e / 4) + 4 * (l / 32) + e % 4, r = r0 + rb * 32 + l % 32;
-        if (t >= a.n || r >= a.out) continue;
+        if (t >= a.n || r >= part.out) continue;
         float y = sums[o];
 #pragma unroll
         for (int g = 1; g < G::KG; ++g) y += sums[g * BLOCKS * 1024 + o];
-        if (FMT == AMK_WEIGHTS_W8A16) y *= ((const float*)a.scale)[r];
-        put<decltype(bf16)::value, decltype(add)::value>(a, t * a.y_stride + r, y);
+        if (FMT == AMK_WEIGHTS_W8A16) y *= ((const float*)part.scale)[r];
+        put<decltype(bf16)::value, decltype(add)::value>(part.y, t * a.y_stride + r, y);
       }
     });
   }
 }
 
+int64_t row_tiles(const LinearArgs& a, int rows) {
+  int64_t tiles = 0;
+  for (int i = 0; i < a.parts; ++i) tiles += (a.part[i].out + rows - 1) / rows;
+  return tiles;
+}
+
 template <int FMT, typename G>
 int launch_tile(const LinearArgs& a, hipStream_t st) {
-  const int tt = (a.n + G::BT - 1) / G::BT, rt = (a.out + G::BR - 1) / G::BR;
+  const int tt = (a.n + G::BT - 1) / G::BT, rt = (int)row_tiles(a, G::BR);
   const dim3 grid((unsigned)(((int64_t)tt * rt + 7) / 8 * 8));
-  if constexpr (FMT == AMK_WEIGHTS_W4A16 && G::BKW <= 64) {
-    if (a.group == 32) {
-      hipLaunchKernelGGL((linear_kernel<FMT, G, true>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
-      return hipGetLastError() == hipSuccess ? AMK_OK : AMK_ERR_DEVICE;
-    }
-  }
-  hipLaunchKernelGGL((linear_kernel<FMT, G, false>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
-  return hipGetLastError() == hipSuccess ? AMK_OK : AMK_ERR_DEVICE;
+  auto launch = [&](auto group32) {
+    constexpr bool G32 = decltype(group32)::value;
+    if (a.parts > 1) hipLaunchKernelGGL((linear_kernel<FMT, G, G32, true>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
+    else hipLaunchKernelGGL((linear_kernel<FMT, G, G32, false>), grid, dim3(G::THREADS), 0, st, a, tt, rt);
+    return hipGetLastError() == hipSuccess ? AMK_OK : AMK_ERR_DEVICE;
+  };
+  if constexpr (FMT == AMK_WEIGHTS_W4A16 && G::BKW <= 64)
+    if (a.group == 32) return launch(std::true_type());
+  return launch(std::false_type());
 }
 
 template <int FMT>
 int launch_fmt(const LinearArgs& a, hipStream_t st) {
   constexpr bool W4 = FMT == AMK_WEIGHTS_W4A16;
-  const int64_t t32 = (int64_t)((a.n + 31) / 32) * ((a.out + 31) / 32);
-  const int64_t t64 = (int64_t)((a.n + 63) / 64) * ((a.out + 63) / 64);
-  const int64_t t128 = (int64_t)((a.n + 127) / 128) * ((a.out + 127) / 128);
-  const int64_t t256 = (int64_t)((a.n + 255) / 256) * ((a.out + 255) / 256);
+  const int64_t t32 = (int64_t)((a.n + 31) / 32) * row_tiles(a, 32);
+  const int64_t t64 = (int64_t)((a.n + 63) / 64) * row_tiles(a, 64);
+  const int64_t t128 = (int64_t)((a.n + 127) / 128) * row_tiles(a, 128);
+  const int64_t t256 = (int64_t)((a.n + 255) / 256) * row_tiles(a, 256);
   // Few tokens, or too few tiles of 128 x 128: small tiles, their columns over 4 to 16 waves.
   // Stages of bf16 and int8 come in rings of three (30 tokens 14336 -> 4096 bf16 41 us, with two
   // 54); those of int4 wait for their scales (see linear_kernel), and where a CU takes one

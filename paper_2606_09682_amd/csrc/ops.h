@@ -11,16 +11,23 @@
 
 namespace amk {
 
+// One of the matrices a launch multiplies the same x with.
+struct LinearPart {
+  const void* w;
+  const void* scale;
+  void* y;
+  int32_t out;
+};
+
 struct LinearArgs {
   const uint16_t* x;
   int64_t x_stride;
-  int32_t n, in, out;
-  const void* w;
-  const void* scale;
+  int32_t n, in;
+  LinearPart part[3];
+  int32_t parts;      // of them used
   int32_t fmt;
   int32_t group;      // W4A16: columns per scale
-  void* y;
-  int64_t y_stride;
+  int64_t y_stride;   // of every y
   int32_t y_bf16, accumulate;
 };
 

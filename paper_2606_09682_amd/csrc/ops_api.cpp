@@ -60,9 +60,10 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
   if (weight_format != AMK_WEIGHTS_BF16 && (!scale || !aligned(scale, w4 ? 2 : 4))) return AMK_ERR_INVALID_ARGUMENT;
   if (out > 1 << 26 || ((int64_t)n + 127) / 128 * (((int64_t)out + 127) / 128) > kMostThreads / 512)
     return AMK_ERR_UNSUPPORTED;
-  LinearArgs a;
-  a.x = (const uint16_t*)x; a.x_stride = x_stride; a.n = n; a.in = in; a.out = out; a.w = w; a.scale = scale;
-  a.fmt = weight_format; a.group = group; a.y = y; a.y_stride = y_stride; a.y_bf16 = y_type == AMK_BF16;
+  LinearArgs a = {};
+  a.x = (const uint16_t*)x; a.x_stride = x_stride; a.n = n; a.in = in;
+  a.part[0] = {w, scale, y, out}; a.parts = 1;
+  a.fmt = weight_format; a.group = group; a.y_stride = y_stride; a.y_bf16 = y_type == AMK_BF16;
   a.accumulate = accumulate;
   return launch_linear(a, stream);
 }
