@@ -37,13 +37,14 @@ SHAPES = {
                                     n_layers=2, vocab=515),
     "tied": synth.get("tiny").with_(name="tied", n_heads=7, n_kv_heads=1, hidden=352, intermediate=416, n_layers=3,
                                     vocab=1001, tied_embeddings=True),
+    "wide": synth.get("tiny").with_(name="wide", n_heads=4, n_kv_heads=2, hidden=256, intermediate=8192, n_layers=1,
+                                    vocab=257),
 }
 
 
-def make(amk, name, fmt, max_seq, static=False):
+def make(amk, name, fmt, max_seq, static=False, group=32):
     cfg = SHAPES[name]
     w = synth.make_weights(cfg, seed=0)
-    group = 32
     if fmt == "w8a16":
         synth.add_w8a16(w)
     elif fmt == "w4a16":
@@ -80,7 +81,7 @@ def oracle_prompt(model, tokens, pos, kv):
     return np.stack([oracle.decode_step(model, int(t), pos + i, kv) for i, t in enumerate(tokens)])
 
 
-@pytest.mark.parametrize("name", sorted(SHAPES))
+@pytest.mark.parametrize("name", ["d128", "tied", "tiny"])
 @pytest.mark.parametrize("fmt", ["bf16", "w8a16", "w4a16"])
 @pytest.mark.parametrize("pos,n", [(0, 1), (0, 37), (5, 64), (0, 65), (9, 131)])
 def test_prompt(env, name, fmt, pos, n):
@@ -103,6 +104,28 @@ def test_prompt(env, name, fmt, pos, n):
     dec.step(tokens[pos + n], pos + n, kv, logits)
     check_logits(cfg, logits.cpu().numpy()[None], ref[-1:])
     assert dec.status() == amk.AMK_OK
+    dec.close()
+
+
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("w8a16", 0), ("w4a16", 32), ("w4a16", 64), ("w4a16", 128)])
+def test_prompts_of_many_tiles(env, fmt, group):
+    """Q, K and V, and gate and up, are multiplied in one launch each, in tiles by the number of tokens: prompts of
+    each kind of tile give what pieces of 20 tokens do, and those what the oracle gives."""
+    amk, torch = env
+    cfg, dec, model = make(amk, "wide", fmt, 2048, group=group)
+    tokens = [int(t) for t in np.random.RandomState(6).randint(0, cfg.vocab, 2048)]
+    kv, ref_kv = kv_to_device(empty_cache(cfg, 2048)), empty_cache(cfg, 2048)
+    small = torch.cat([dec.extend(tokens[i:i + 20], i, kv) for i in range(0, 2048, 20)]).cpu().numpy()
+    check_logits(cfg, small[:30], oracle_prompt(model, tokens[:30], 0, ref_kv))
+    small_rows = rows_of(kv_from_device(kv), 0, 2048)
+    check_rows(cfg, small_rows[:, :, :, :30], rows_of(ref_kv, 0, 30))
+    for n in (100, 150, 300, 2048):  # each side may be off by the share
+        kv.zero_()
+        got = dec.extend(tokens[:n], 0, kv).cpu().numpy()
+        rows = rows_of(kv_from_device(kv), 0, n)
+        assert np.all(np.abs(got - small[:n]).max(-1) <= 2 * share(cfg) * np.abs(small[:n]).max(-1))
+        top = np.abs(small_rows[:, :, :, :n]).max(-1)
+        assert np.all(np.abs(rows - small_rows[:, :, :, :n]).max(-1) <= 2 * (share(cfg) + 2.0 ** -8) * top)
     dec.close()
 
 
