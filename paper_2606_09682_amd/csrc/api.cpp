@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -63,6 +64,9 @@ struct amk_handle_s {
   int32_t* d_words = nullptr;   // static handles: status at [0], abort at [16]
   void* last_stream = nullptr;
   bool launched = false;
+  // amk_extend has enqueued work that reads the device block and the weights, on streams
+  // that are not kept (several calls may run at once): destroying waits for the device
+  std::atomic<bool> extended{false};
   uint64_t timeout_ticks = 0;
   // the last kv_cache / logits pointers found to be device memory of this
   // device with room for a step's accesses (the check is skipped while the
@@ -120,7 +124,7 @@ void release_static(int device, amk_handle_s* h) {
 void free_handle(amk_handle_s* h) {
   if (!h) return;
   DeviceGuard g(h->device);
-  if (h->launched) (void)hipDeviceSynchronize();
+  if (h->launched || h->extended) (void)hipDeviceSynchronize();
   if (h->is_static) release_static(h->device, h);
   else if (h->d_block) (void)hipFree(h->d_block);
   if (h->h_status) (void)hipHostFree(h->h_status);
@@ -709,6 +713,7 @@ int amk_extend(amk_handle_t h, const int32_t* tokens, int32_t n, int32_t pos, co
       !device_range(kv_cache, amk_kv_cache_bytes_of(s), h->device) ||
       (n_logits && !device_range(logits, sizeof(float) * (size_t)s.V * n_logits, h->device)))
     return AMK_ERR_INVALID_ARGUMENT;
+  h->extended = true;
 
   char* base = (char*)workspace;
   float* x = (float*)(base + lay.x);
