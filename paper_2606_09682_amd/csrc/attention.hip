@@ -269,11 +269,13 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
     for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
   top = fmaxf(top, __shfl_xor(top, 32));
   // m follows the maximum only where a score exceeds it by 2^8: sums and products lose
-  // nothing by weights of up to 256, and most tiles need not rescale O
+  // nothing by weights of up to 256, and most tiles need not rescale O.  Each row goes by
+  // its own scores: what another row of the wave sees does not move its m
   const float high = top * scale2;
-  if (__any(high > run.m + 8.f)) {
-    const float m = fmaxf(run.m, high);
-    const float keep = __builtin_amdgcn_exp2f(run.m - (m == -INFINITY ? 0.f : m));
+  const bool moves = high > run.m + 8.f;
+  if (__any(moves)) {
+    const float m = moves ? high : run.m;
+    const float keep = moves ? __builtin_amdgcn_exp2f(run.m - m) : 1.f;
     run.m = m;
     run.l *= keep;
 #pragma unroll

@@ -1,4 +1,5 @@
-"""Edges of the operators for several tokens: handles destroyed with work under way."""
+"""Edges of the operators for several tokens: handles destroyed with work under way, attention rows whose bits
+depend on nothing that they do not see."""
 import numpy as np
 import pytest
 
@@ -20,6 +21,46 @@ def env():
         build.build()
     amk.load()
     return amk, torch
+
+
+def randn(torch, seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+# ---- attention -----------------------------------------------------------------------------
+HEADS = [(1, 1, 64), (8, 1, 64), (6, 2, 128), (32, 8, 128), (128, 1, 128)]
+
+
+@pytest.mark.parametrize("heads,kv,d", HEADS)
+@pytest.mark.parametrize("key", [45, 101, 198])
+def test_prompt_rows_before_a_high_score(env, heads, kv, d, key):
+    """A finite key that scores far above all others moves the running maximum of the rows that see it. The rows
+    before it, some of them in the same wave, give the same bits with it and without."""
+    amk, torch = env
+    for seed in range(4):
+        q = (randn(torch, seed, 230, heads, d) + 1).to(torch.bfloat16)
+        k, v = (randn(torch, seed + s, 230, kv, d).to(torch.bfloat16) for s in (10, 20))
+        clean = amk.prompt_attention(q, k, v)
+        k[key] = 8.0
+        got = amk.prompt_attention(q, k, v)
+        assert torch.equal(got[:key], clean[:key])
+        assert not torch.equal(got[key:], clean[key:])
+
+
+@pytest.mark.parametrize("heads,kv,d", HEADS)
+@pytest.mark.parametrize("n,pos", [(12, 10), (40, 300), (64, 3000)])
+def test_tree_branches_beside_a_high_score(env, heads, kv, d, n, pos):
+    """A token of one branch that scores far above all others: the other branch has the same bits."""
+    amk, torch = env
+    masks = [1 << i | sum(1 << j for j in range(i % 2, i, 2)) for i in range(n)]  # of odd and of even tokens
+    for seed in range(4):
+        q = (randn(torch, seed, n, heads, d) + 1).to(torch.bfloat16)
+        k, v = (randn(torch, seed + s, pos + n, kv, d).to(torch.bfloat16) for s in (10, 20))
+        clean = amk.tree_attention(q, k, v, pos, masks)
+        k[pos + 7] = 8.0
+        got = amk.tree_attention(q, k, v, pos, masks)
+        assert torch.equal(got[0::2], clean[0::2])
+        assert not torch.equal(got[7::2], clean[7::2])
 
 
 # ---- handles -------------------------------------------------------------------------------
