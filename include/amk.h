@@ -330,9 +330,10 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
  * finite) multiplies the scores, usually 1 / sqrt(head_dim).  At most 2^30 rows of k
  * and 2^30 pairs of a token and a query head.
  * Scores, softmax statistics and the weighted sums are fp32; weights are
- * rounded to bf16 for the product with v.  A row that sees no key, or only keys
- * scoring minus infinity, gets zeros; what a row does not see never reaches it,
- * infinities and NaN included. */
+ * rounded to bf16 for the product with v.  A key scoring minus infinity counts as
+ * not seen, and a row that sees no key gets zeros; what a row does not see never
+ * reaches it, not even its last bit, infinities and NaN included.  An infinity or
+ * NaN in v reaches every row that sees its key, however small the weight. */
 typedef struct {
   const void* q;
   const void* k;

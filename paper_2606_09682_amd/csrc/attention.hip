@@ -26,10 +26,13 @@
 // (32 rows at one column) nor the transposed V reads (4 rows x 32 bytes) meet in
 // a bank.
 //
-// Masked keys.  A score outside a row's keys is replaced, not added to.  p is
-// then 0, but 0 * V is NaN where V holds an infinity or NaN, so in tiles that
-// some row sees only in part such values of V are set to 0 before the product;
-// if there were any, they are added at the end to the rows that see their key.
+// Masked keys.  A score outside a row's keys is replaced, not added to, and p is then 0.
+//
+// Infinities and NaN of V.  0 * V is NaN there, and whether a small p is 0 depends on where
+// the tiles begin.  A row whose O is not finite has its workgroup go through its tiles once
+// more, with such values of V counted as 0, and adds them afterwards itself: those whose
+// key it sees with any score but minus infinity, as their weight is then above 0 however
+// small.  Rows that see none of them get the bits they have without them.
 //
 // What bounds it.  The two waves of a SIMD take turns at products and softmax: at a
 // prompt of 8192 tokens, 32 query and 8 KV heads of 128, the matrix cores are busy 51%
@@ -41,6 +44,7 @@
 // Eight tokens at 300, 9 and 3 heads of 64, take 8.5 us, ten tiles one after another.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -213,19 +217,22 @@ template <int HD>
 struct Running {
   f32x16 o[HD / 32];
   float m, l;
-  int odd;  // values of V were set to 0
 };
 
+// Rows see all keys of a tile, or some only (PARTIAL); CLEAN: PARTIAL, and infinities and NaN
+// of V count as 0.
+enum class Keys { WHOLE, PARTIAL, CLEAN };
+
 // Takes tile t, which lies in kt and vt, into the running result, while tile t + 1 (if
-// more follow) is loaded into `next`.  PARTIAL: some row sees only some of the keys.
-// kt, vt, next and odd do not overlap: without that promise, which the compiler follows for
-// pointers of few uses only, every read of tile t would wait for the loads of tile t + 1.
-template <int HD, int WAVES, int BN, bool PARTIAL>
-__device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int t, bool more,
+// more follow) is loaded into `next`.  kt, vt and next do not overlap: without that promise,
+// which the compiler follows for pointers of few uses only, every read of tile t would wait
+// for the loads of tile t + 1.  Returns whether (under CLEAN) this thread set values to 0.
+template <int HD, int WAVES, int BN, Keys KEYS>
+__device__ __forceinline__ bool attn_step(const Source<HD, WAVES, BN>& from, int t, bool more,
                                           const AMK_LDS uint16_t* __restrict__ kt,
                                           AMK_LDS uint16_t* __restrict__ vt, AMK_LDS uint16_t* __restrict__ next,
-                                          AMK_LDS int* __restrict__ odd, const bf16x8* q, const Sees& sees,
-                                          int kend, float scale2, Running<HD>& run) {
+                                          const bf16x8* q, const Sees& sees, int kend, float scale2,
+                                          Running<HD>& run) {
   constexpr int KB = BN / 32, DB = HD / 32;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   if (more) from.tile(t + 1, next);
@@ -240,7 +247,7 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
       sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], sc[kb], 0, 0, 0);
     }
 
-  if constexpr (!PARTIAL) {
+  if constexpr (KEYS == Keys::WHOLE) {
     // K's operands are read four ahead of the products that take them (0x100: LDS reads, 8:
     // matrix instructions)
     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
@@ -252,7 +259,7 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
   }
 
-  if constexpr (PARTIAL) {
+  if constexpr (KEYS != Keys::WHOLE) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const uint32_t word = sees.word(t * BN + kb * 32, kend) >> 4 * half;
@@ -292,7 +299,8 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
       run.l += sc[kb][i];
     }
 
-  if constexpr (PARTIAL) {
+  bool odd = false;
+  if constexpr (KEYS == Keys::CLEAN) {
 #pragma unroll
     for (int i = 0; i < Source<HD, WAVES, BN>::LOADS; ++i) {
       AMK_LDS u32x4* at = (AMK_LDS u32x4*)vt + i * 64 * WAVES + threadIdx.x;
@@ -305,10 +313,9 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
         x[e] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
       }
       if (here) *at = x;
-      if (here) *odd = 1;
+      odd |= here;
     }
     __syncthreads();
-    run.odd |= *odd;
   }
 
   bf16x8 p[KB][2];
@@ -329,17 +336,55 @@ __device__ __forceinline__ void attn_step(const Source<HD, WAVES, BN>& from, int
         const s16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         run.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), p[kb][ks], run.o[d], 0, 0, 0);
       }
+  return odd;
+}
+
+// Adds the infinities and NaN of V at keys [key, end) to the rows that see their key with a
+// score other than minus infinity.  Rare: a lane takes its row's key by key.
+template <int HD, typename Source>
+__device__ __forceinline__ void add_odd(const Source& from, int key, int end, const bf16x8* q, const Sees& sees,
+                                        int half, Running<HD>& run) {
+  for (; key < end; ++key) {
+    const unsigned char* kp = from.k + key * from.k_row + half * 16;
+    float score = 0.f;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) {
+      const u32x4 a = __builtin_bit_cast(u32x4, q[i]), b = *(const u32x4*)(kp + 32 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t qw = a[e], kw = b[e];
+        score = __builtin_fmaf(bf16_to_f32((uint16_t)qw), bf16_to_f32((uint16_t)kw), score);
+        score = __builtin_fmaf(bf16_to_f32((uint16_t)(qw >> 16)), bf16_to_f32((uint16_t)(kw >> 16)), score);
+      }
+    }
+    score += __shfl_xor(score, 32);
+    if (!(sees.word(key, end) & 1) || score == -INFINITY) continue;
+    const uint16_t* vp = (const uint16_t*)(from.v + key * from.v_row) + 4 * half;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x2 w = *(const u32x2*)(vp + 32 * d + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t word = w[e / 2];
+          const float x = bf16_to_f32((uint16_t)(word >> e % 2 * 16));
+          if (!(fabsf(x) < INFINITY)) run.o[d][4 * i + e] += x;
+        }
+      }
+  }
 }
 
 template <int HD, int WAVES, int BN, typename Which>
 __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, const Which w) {
   constexpr int ROWS = 32 * WAVES, DB = HD / 32;
   constexpr int TILE = BN * HD;  // elements of a K or V tile
-  // two stages of K and V and a flag: one variable, since the compiler keeps what it knows
-  // of attn_step's pointers only where a kernel has no second one
+  // two stages of K and V and a note of what is rare: one variable, since the compiler keeps
+  // what it knows of attn_step's pointers only where a kernel has no second one
   __shared__ __align__(16) uint16_t lds[4 * TILE + 8];
   AMK_LDS uint16_t* stages = (AMK_LDS uint16_t*)lds;
-  AMK_LDS int* odd = (AMK_LDS int*)(stages + 4 * TILE);
+  // [0] a row is not finite; V's infinities and NaN lie in tiles [1] .. below [2]
+  AMK_LDS int* note = (AMK_LDS int*)(stages + 4 * TILE);
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int half = lane >> 5, col = lane & 31;
@@ -377,39 +422,57 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
   const int tf = max(t0, min(t1, kfull / BN));  // tiles that every row sees whole
   const Source<HD, WAVES, BN> from(a.k + s.k0 * a.k_token + kvh * a.k_head, a.v + s.k0 * a.v_token + kvh * a.v_head,
                                    a.k_token, a.v_token, s.nk);
-  if (threadIdx.x == 0) *odd = 0;
-  Running<HD> run = {};
-  run.m = -INFINITY;
-  if (t0 < t1) from.tile(t0, stages);
-  int t = t0, stage = 0;
-  for (; t < tf; ++t, stage ^= 1) {
-    stage_barrier<0>();  // tile t is in, and the readers of the other stage are done
-    AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
-    attn_step<HD, WAVES, BN, false>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE,
-                                    odd, q, sees, kend, a.scale2, run);
+  if (threadIdx.x == 0) {
+    note[0] = 0;
+    note[1] = t1;
+    note[2] = t0;
   }
-  for (; t < t1; ++t, stage ^= 1) {
-    stage_barrier<0>();
-    AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
-    attn_step<HD, WAVES, BN, true>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE, odd,
-                                   q, sees, kend, a.scale2, run);
-  }
-
-  if (run.odd) {  // rare: add what was set to 0 to the rows that see it
-    for (int key = tf * BN; key < min(t1 * BN, kend); ++key) {
-      if (!(sees.word(key, kend) & 1)) continue;
-      const uint16_t* vp = (const uint16_t*)(from.v + key * from.v_row) + 4 * half;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = bf16_to_f32(vp[32 * d + 8 * (i / 4) + i % 4]);
-          if (!(fabsf(x) < INFINITY)) run.o[d][i] += x;
-        }
+  Running<HD> run;
+  auto pass = [&](auto keys) {
+    constexpr Keys KEYS = decltype(keys)::value;
+    run = {};
+    run.m = -INFINITY;
+    int first = t1, past = t0, t = t0, stage = 0;  // tiles in which this thread set values of V to 0
+    if (t0 < t1) from.tile(t0, stages);
+    if constexpr (KEYS == Keys::PARTIAL)
+      for (; t < tf; ++t, stage ^= 1) {
+        stage_barrier<0>();  // tile t is in, and the readers of the other stage are done
+        AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
+        attn_step<HD, WAVES, BN, Keys::WHOLE>(from, t, t + 1 < t1, cur, cur + TILE, stages + (stage ^ 1) * 2 * TILE, q,
+                                              sees, kend, a.scale2, run);
+      }
+    for (; t < t1; ++t, stage ^= 1) {
+      stage_barrier<0>();
+      AMK_LDS uint16_t* cur = stages + stage * 2 * TILE;
+      const bool odd = attn_step<HD, WAVES, BN, KEYS>(from, t, t + 1 < t1, cur, cur + TILE,
+                                                      stages + (stage ^ 1) * 2 * TILE, q, sees, kend, a.scale2, run);
+      if (KEYS == Keys::CLEAN && odd) {
+        first = min(first, t);
+        past = t + 1;
+      }
     }
+    if (KEYS == Keys::CLEAN && first < past) {
+      __hip_atomic_fetch_min(note + 1, first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      __hip_atomic_fetch_max(note + 2, past, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+  };
+  pass(std::integral_constant<Keys, Keys::PARTIAL>());
+  float l = run.l + __shfl_xor(run.l, 32);
+  float zero = 0.f;  // NaN if O holds an infinity or NaN
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(run.o[d][i], 0.f, zero);
+  // a row whose sum is NaN stays NaN
+  if (valid && l == l && zero != zero) note[0] = 1;
+  __syncthreads();
+  if (note[0]) {
+    pass(std::integral_constant<Keys, Keys::CLEAN>());
+    l = run.l + __shfl_xor(run.l, 32);
+    __syncthreads();
+    add_odd<HD>(from, note[1] * BN, min(note[2] * BN, kend), q, sees, half, run);
   }
 
-  const float l = run.l + __shfl_xor(run.l, 32);
   if (!valid) return;
   if (a.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -438,7 +501,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attn_kernel(const AttnArgs a, c
 
 // Joins the splits of each (token, head), one wave each: HD / 4 lanes take a split's row
 // of O, so 2 or 4 splits are read side by side and 8 or 16 are on their way.  Splits
-// that saw nothing for the row (l = 0) are left out.
+// that saw nothing for the row (l = 0) are left out; the infinities and NaN of any other
+// stay, also where its weight is too small for fp32.
 template <int HD>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, const int32_t* cu_q, int32_t n_seqs) {
   constexpr int LANES = HD / 4, SIDE = 64 / LANES, AHEAD = 4;
@@ -456,11 +520,13 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, const 
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   const float* po = a.part_o + at * HD + lane % LANES * 4;
   for (int i0 = 0; i0 < a.splits; i0 += 64) {
-    float f = 0.f;
+    float f = -1.f;  // left out
     if (i0 + lane < a.splits) {
       const float2 ml = a.part_ml[(i0 + lane) * all + at];
-      if (ml.y != 0.f) f = __builtin_amdgcn_exp2f(ml.x - base);
-      l += f * ml.y;
+      if (ml.y != 0.f) {
+        f = __builtin_amdgcn_exp2f(ml.x - base);
+        l += f * ml.y;
+      }
     }
     const int n = min(64, a.splits - i0);
     for (int i = 0; i < n; i += SIDE * AHEAD) {
@@ -470,12 +536,15 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, const 
       for (int u = 0; u < AHEAD; ++u) {
         const int k = i + u * SIDE + sub;
         w[u] = __shfl(f, k & 63);
-        if (k >= n) w[u] = 0.f;
+        if (k >= n) w[u] = -1.f;
         v[u] = *(const f32x4*)(po + (int64_t)(i0 + min(k, n - 1)) * all * HD);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
-        if (w[u] != 0.f) o += w[u] * v[u];
+        if (w[u] > 0.f) o += w[u] * v[u];
+        else if (w[u] == 0.f)
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(v[u][e]) < INFINITY)) o[e] += v[u][e];
     }
   }
   for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);

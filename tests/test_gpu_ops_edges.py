@@ -1,5 +1,7 @@
 """Edges of the operators for several tokens: handles destroyed with work under way, attention rows whose bits
-depend on nothing that they do not see."""
+depend on nothing that they do not see, infinities and NaN in V."""
+import math
+
 import numpy as np
 import pytest
 
@@ -61,6 +63,81 @@ def test_tree_branches_beside_a_high_score(env, heads, kv, d, n, pos):
         got = amk.tree_attention(q, k, v, pos, masks)
         assert torch.equal(got[0::2], clean[0::2])
         assert not torch.equal(got[7::2], clean[7::2])
+
+
+def odd_inputs(torch, seed, n, rows, heads, kv, d):
+    """q [n], k, v [rows], every query's first element 1: k[j] = (x, 0, 0, ...) scores x for all."""
+    q = randn(torch, seed, n, heads, d).to(torch.bfloat16)
+    q[:, :, 0] = 1
+    k, v = (randn(torch, seed + s, rows, kv, d).to(torch.bfloat16) for s in (10, 20))
+    return q, k, v
+
+
+def calls_of(amk, torch, q, k, v):
+    """Attentions of the last queries to k's rows: as a prompt and (up to 64) as a chain: {name: result}"""
+    n = q.shape[0]
+    out = {"prompt": amk.prompt_attention(q, k, v)}
+    if n <= 64:
+        out["tree"] = amk.tree_attention(q, k, v, k.shape[0] - n, [(2 << i) - 1 for i in range(n)])
+    return out
+
+
+# queries, keys, and the key in question: in tiles that all rows see whole, in those of the diagonal, in ranges
+# of keys that are split
+ODD = [(200, 200, 20), (200, 200, 77), (90, 90, 0), (300, 300, 131), (40, 340, 100), (40, 340, 305), (12, 3012, 100),
+       (60, 4060, 4010), (1, 3000, 1500), (1, 31, 30)]
+
+
+@pytest.mark.parametrize("heads,kv,d", [(1, 1, 64), (6, 2, 64), (8, 1, 128), (128, 1, 128)])
+@pytest.mark.parametrize("n,rows,key", ODD)
+def test_odd_values_of_keys_without_weight(env, heads, kv, d, n, rows, key):
+    """A key that scores minus infinity has no weight: what its V holds reaches no row, wherever tiles begin."""
+    amk, torch = env
+    q, k, v = odd_inputs(torch, 1, n, rows, heads, kv, d)
+    k[key], k[key, :, 0] = 0, -math.inf
+    clean = calls_of(amk, torch, q, k, v)
+    for bad in (math.inf, -math.inf, math.nan):
+        v[key, :, 5], v[key, :, d - 1] = bad, -bad
+        for name, got in calls_of(amk, torch, q, k, v).items():
+            assert torch.equal(got, clean[name]), (name, bad)
+
+
+@pytest.mark.parametrize("heads,kv,d", [(1, 1, 64), (6, 2, 64), (8, 1, 128), (128, 1, 128)])
+@pytest.mark.parametrize("n,rows,key", ODD)
+@pytest.mark.parametrize("score", [0.0, -3e4])
+def test_odd_values_reach_the_rows_that_see_them(env, heads, kv, d, n, rows, key, score):
+    """However small a key's weight (2^-5000 here), an infinity or NaN of its V reaches every row that sees it, in
+    its own column; all other rows and columns keep their bits."""
+    amk, torch = env
+    q, k, v = odd_inputs(torch, 2, n, rows, heads, kv, d)
+    k[key], k[key, :, 0] = 0, score
+    clean = calls_of(amk, torch, q, k, v)
+    before = max(0, key - (rows - n))  # queries that do not see the key
+    others = [c for c in range(d) if c != 5]
+    for bad in (math.inf, -math.inf, math.nan):
+        v[key, :, 5] = bad
+        for name, got in calls_of(amk, torch, q, k, v).items():
+            assert torch.equal(got[:before], clean[name][:before]), (name, bad)
+            assert torch.equal(got[before:, :, others], clean[name][before:, :, others]), (name, bad)
+            seen = got[before:, :, 5].float()
+            assert bool(torch.isnan(seen).all() if math.isnan(bad) else (seen == bad).all()), (name, bad)
+    if rows - n <= key < rows - 1:  # opposite infinities have no sum; query `before` is the last without the second
+        v[key, :, 5], v[key + 1, :, 5] = math.inf, -math.inf
+        for name, got in calls_of(amk, torch, q, k, v).items():
+            assert (got[before, :, 5] == math.inf).all() and torch.isnan(got[before + 1:, :, 5]).all()
+
+
+def test_rows_of_keys_without_weight_are_zeros(env):
+    """Rows whose keys all score minus infinity get zeros, with infinities and NaN in V too; longer rows go on."""
+    amk, torch = env
+    for d, n in ((64, 150), (128, 150), (128, 64)):
+        for none in (3, 64, 100):
+            q, k, v = odd_inputs(torch, 3, n, n, 4, 2, d)
+            k[:none], k[:none, :, 0] = 0, -math.inf
+            clean = calls_of(amk, torch, q, k, v)
+            v[:none:2], v[1:none:2] = math.inf, math.nan
+            for name, got in calls_of(amk, torch, q, k, v).items():
+                assert (got[:none] == 0).all() and torch.equal(got, clean[name])
 
 
 # ---- handles -------------------------------------------------------------------------------
