@@ -26,7 +26,7 @@
 // What bounds it.  2048 tokens 4096 -> 14336: matrix cores (busy 55% of the time; 448
 // tiles of 256 x 256 are 1.75 rounds of the CUs), bf16 232 us, 1035 TFLOP/s (the library's
 // product 208, a large square one 1380); int8 240; int4, which also converts and scales
-// sums, 305.  32 tokens 4096 -> 14336: bf16 27 us (4.4 TB/s), int8 13.7, int4 13.9: with
+// sums, 300.  32 tokens 4096 -> 14336: bf16 27 us (4.4 TB/s), int8 13.7, int4 13.9: with
 // the smaller formats the copies of x that every tile reads from L2, 117 MB, weigh more
 // than the weights.  5 tokens int8 576 -> 1536 take 3.6 us, hardly more than a launch.
 #include <type_traits>
@@ -54,25 +54,28 @@ __device__ __forceinline__ bf16x8 int8_to_bf16(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// The 8 codes of one packed int4 word (low nibbles are columns 0..3, high ones 4..7) as
-// (c + 8) * 2^-9: a byte 0..15 read as FP8 E4M3 is that number of steps of its subnormals.
-// Half the work of a conversion through fp32; the 8 comes off as a product with kEight.
+// The 8 codes of one packed int4 word as bf16 (low nibbles are columns 0..3, high ones 4..7;
+// a nibble u stands for c = u - 8).  A byte of a sign and |c| <= 8, read as FP8 E4M3, is c
+// steps of its subnormals (8 is the first normal number), 2^-9 each, which the conversion's
+// scale makes 1: less work than a conversion through fp32.
 __device__ __forceinline__ bf16x8 int4_to_bf16(uint32_t w) {
-  const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
+  const uint32_t sign = ~w & 0x88888888u;            // of each nibble
+  const uint32_t neg = sign >> 3;
+  const uint32_t mag = (w ^ (0x88888888u - neg)) + neg;  // u - 8, or (u ^ 7) + 1 = 8 - u: within the nibble
+  const uint32_t lo = (mag & 0x0f0f0f0fu) | ((sign << 4) & 0xf0f0f0f0u);
+  const uint32_t hi = ((mag >> 4) & 0x0f0f0f0fu) | (sign & 0xf0f0f0f0u);
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   u32x4 r;
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, true);
   r[0] = __builtin_bit_cast(uint32_t, a);
   r[1] = __builtin_bit_cast(uint32_t, b);
   r[2] = __builtin_bit_cast(uint32_t, c);
   r[3] = __builtin_bit_cast(uint32_t, d);
   return __builtin_bit_cast(bf16x8, r);
 }
-constexpr uint32_t kEight = 0xbc80bc80u;  // two bf16 of -8 * 2^-9
-constexpr float kStep = 512.f;            // 2^9, in the scales
 
 template <int FMT, int TB_, int RB_, int WT_, int WR_, int KG_, int BKW_, int STAGES_ = 2, int XR_ = 32 * TB_ * WT_>
 struct Tile {
@@ -187,8 +190,11 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
   xs += (kg * G::XR + wt * 32 * G::TB + xrow) * G::XC * 16;
   ws += (kg * G::BR + wr * 32 * G::RB + col) * G::WC * 16;
   const bf16x8 nothing = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
-  const bf16x8 eight = __builtin_bit_cast(bf16x8, u32x4{kEight, kEight, kEight, kEight});
-  auto read_x = [&](int u, bf16x8 (&xf)[G::TB][2]) {
+  constexpr int US = G::BKW / 32, SPAN = GROUP32 ? 1 : US;  // slices, and those of one group
+  f32x16 part[G::TB][G::RB];  // W4A16: the sums of a group of columns
+#pragma unroll
+  for (int u = 0; u < US; ++u) {
+    bf16x8 xf[G::TB][2], wf[G::RB][2];
 #pragma unroll
     for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
@@ -197,32 +203,12 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
         xf[tb][s] = *(const AMK_LDS bf16x8*)(xs + 32 * tb * G::XC * 16 + c * 16);
         if (TAIL && kw + 32 * u + 16 * half + 8 * s >= in) xf[tb][s] = nothing;
       }
-  };
-  // W4A16: the sums of a group of columns.  They begin with -8 times those of x, which
-  // are the same for all rows of W.
-  constexpr int US = G::BKW / 32, SPAN = GROUP32 ? 1 : US;  // slices, and those of one group
-  f32x16 part[G::TB][G::RB];
-  bf16x8 xf[W4 ? SPAN : 1][G::TB][2];
+    if constexpr (W4)
+      if (u % SPAN == 0)
 #pragma unroll
-  for (int u = 0; u < US; ++u) {
-    bf16x8 wf[G::RB][2];
-    if constexpr (W4) {
-      if (u % SPAN == 0) {
+        for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
-        for (int i = 0; i < SPAN; ++i) read_x(u + i, xf[i]);
-#pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb) {
-          f32x16 off = {};
-#pragma unroll
-          for (int i = 0; i < 2 * SPAN; ++i)
-            off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[i / 2][tb][i % 2], eight, off, 0, 0, 0);
-#pragma unroll
-          for (int rb = 0; rb < G::RB; ++rb) part[tb][rb] = off;
-        }
-      }
-    } else {
-      read_x(u, xf[0]);
-    }
+          for (int rb = 0; rb < G::RB; ++rb) part[tb][rb] = f32x16{};
 #pragma unroll
     for (int rb = 0; rb < G::RB; ++rb) {
       const AMK_LDS unsigned char* wrow = ws + 32 * rb * G::WC * 16;
@@ -251,10 +237,11 @@ __device__ __forceinline__ void linear_step(const Source<G>& from, int in, int k
 #pragma unroll
         for (int rb = 0; rb < G::RB; ++rb) {
           f32x16& sum = W4 ? part[tb][rb] : acc[tb][rb];
-          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[W4 ? u % SPAN : 0][tb][s], wf[rb][s], sum, 0, 0, 0);
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[tb][s], wf[rb][s], sum, 0, 0, 0);
         }
     if constexpr (W4) {
-      if (u % SPAN == SPAN - 1) {
+      // (columns past the last have no scale: 0 times a neighbour's need not be 0)
+      if (u % SPAN == SPAN - 1 && !(TAIL && kw + 32 * (u - SPAN + 1) >= in)) {
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
@@ -286,7 +273,7 @@ __device__ __forceinline__ void by_output(const LinearArgs& a, F f) {
 }
 
 // MANY: more than one matrix.  One alone is read straight from the arguments, since choosing
-// costs its loads their early start (32 tokens int4 4096 -> 14336 14.2 us, chosen 14.7).
+// costs its loads their early start (32 tokens int4 4096 -> 14336 13.9 us, chosen 14.5).
 template <int FMT, typename G, bool GROUP32, bool MANY>
 __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs a, int token_tiles, int row_tiles) {
   __shared__ __align__(16) unsigned char lds[G::LDS];
@@ -352,7 +339,7 @@ __global__ void __launch_bounds__(G::THREADS, 2) linear_kernel(const LinearArgs 
         for (int u = 0; u < (GROUP32 ? G::BKW / 32 : 1); ++u) {
           // with MANY the compiler converts a scale, and so waits for it, where it was loaded
           if constexpr (MANY) asm volatile("" : "+v"(ahead[rb][u]));
-          scale[rb][u] = half_to_f32((uint16_t)ahead[rb][u]) * kStep;
+          scale[rb][u] = half_to_f32((uint16_t)ahead[rb][u]);
         }
     }
     fetch(k0 + G::COLS);
@@ -443,7 +430,7 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
   // Few tokens, or too few tiles of 128 x 128: small tiles, their columns over 4 to 16 waves.
   // Stages of bf16 and int8 come in rings of three (30 tokens 14336 -> 4096 bf16 41 us, with two
   // 54); those of int4 wait for their scales (see linear_kernel), and where a CU takes one
-  // tile, 16 waves on it hide some of that (30 tokens 14336 -> 4096 23.2 us, with 8 26.5).
+  // tile, 16 waves on it hide some of that (30 tokens 14336 -> 4096 23.7 us, with 8 26.6).
   if (a.n <= 16) {  // x is padded to 16 only: 16 tokens bf16 4096 -> 4096 8.3 us, with 32 9.5
     if constexpr (W4)
       if (t32 <= 256) return launch_tile<FMT, Tile<FMT, 1, 1, 1, 1, 16, 64, 2, 16>>(a, st);
@@ -471,7 +458,7 @@ int launch_fmt(const LinearArgs& a, hipStream_t st) {
   const int64_t large = (t256 + 255) / 256 * 10, medium = (t128 + 511) / 512 * 6;
   if constexpr (W4) {
     // where groups allow it, stages of 128 columns: half as many sums to scale, 2048 tokens
-    // 4096 -> 14336 309 us (345 with stages of 64)
+    // 4096 -> 14336 302 us (336 with stages of 64)
     if (a.group >= 128)
       return large <= medium ? launch_tile<FMT, Tile<FMT, 2, 2, 2, 4, 1, 128>>(a, st)
                              : launch_tile<FMT, Tile<FMT, 2, 2, 2, 2, 1, 128>>(a, st);

@@ -1,5 +1,7 @@
-"""Edges of the operators for several tokens: handles destroyed with work under way, attention rows whose bits
-depend on nothing that they do not see, infinities and NaN in V."""
+"""Edges of the operators for several tokens: products of small codes, infinities and few tokens, handles destroyed with work under way, attention rows whose bits
+depend on nothing that they do not see, infinities and NaN in V.
+
+An fp32 sum of k exact products is off by at most k 2^-24 times the sum of their magnitudes, whatever the codes."""
 import math
 
 import numpy as np
@@ -27,6 +29,108 @@ def env():
 
 def randn(torch, seed, *shape):
     return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+# ---- products ------------------------------------------------------------------------------
+def packed(torch, codes):
+    """Codes in [-8, 7] [out, in] in the packed layout: of 8 columns, the low nibbles are the first four."""
+    u = (codes + 8).to(torch.uint8).view(codes.shape[0], -1, 2, 4)
+    return (u[:, :, 0] | u[:, :, 1] << 4).reshape(codes.shape[0], -1).contiguous()
+
+
+def codes_and_scale(torch, seed, low, high, out, width, group):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c = torch.randint(low, high + 1, (out, width), generator=g, device="cuda")
+    return c, (torch.rand(out, width // group, generator=g, device="cuda") * 0.1 + 0.01).half()
+
+
+# tokens, columns, rows, group: every kind of tile, columns that end inside a stage
+TILES = [(1, 256, 40, 64), (9, 544, 8230, 32), (16, 1152, 300, 128), (30, 1056, 130, 32), (31, 1152, 8190, 128),
+         (64, 1088, 4096, 64), (100, 1056, 4096, 32), (200, 1088, 4090, 64), (300, 416, 4090, 32), (511, 640, 4099, 128),
+         (1030, 160, 4100, 32), (2050, 192, 8200, 64), (2050, 384, 2060, 128), (2050, 512, 8200, 256)]
+
+
+@pytest.mark.parametrize("n,width,out,group", TILES)
+def test_int4_codes_are_exact(env, n, width, out, group):
+    """Zero codes give zero; a token of one 1 gives a column's codes times their scales, rounded nowhere; codes of
+    -1, 0 and 1 are summed as closely as any."""
+    amk, torch = env
+    x = randn(torch, n, n, width).to(torch.bfloat16)
+    c, s = codes_and_scale(torch, 1, 0, 0, out, width, group)
+    assert not amk.linear(x, packed(torch, c), s, "w4a16", group).any()
+    c, s = codes_and_scale(torch, 2, -1, 1, out, width, group)
+    w64 = c.double() * s.double().repeat_interleave(group, 1)
+    y = amk.linear(x, packed(torch, c), s, "w4a16", group)
+    tol = (width + 4) * 2.0 ** -24 * (x.double().abs() @ w64.abs().t())
+    assert float(((y.double() - x.double() @ w64.t()).abs() - tol).max()) <= 0
+    c, s = codes_and_scale(torch, 3, -8, 7, out, width, group)
+    w = c.float() * s.float().repeat_interleave(group, 1)
+    at = torch.randint(0, width, (n,), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    one = torch.zeros(n, width, dtype=torch.bfloat16, device="cuda")
+    one[torch.arange(n, device="cuda"), at] = 1
+    assert torch.equal(amk.linear(one, packed(torch, c), s, "w4a16", group), w.t()[at])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "w8a16", "w4a16"])
+@pytest.mark.parametrize("n,width,out,group", TILES)
+def test_infinite_tokens(env, fmt, n, width, out, group):
+    """An infinity in x gives what the product's definition does: an infinity of its weight's sign, NaN where the
+    weight is 0 or two infinities meet; other tokens do not change."""
+    amk, torch = env
+    x = randn(torch, n, n, width).to(torch.bfloat16)
+    c, s = codes_and_scale(torch, 5, -8, 7, out, width, group)
+    if fmt == "bf16":
+        args, w64 = (c.to(torch.bfloat16),), c.double()
+    elif fmt == "w8a16":
+        args, w64 = (c.to(torch.int8), s[:, 0].float().contiguous(), fmt), c.double() * s[:, :1].double()
+    else:
+        args, w64 = (packed(torch, c), s, fmt, group), c.double() * s.double().repeat_interleave(group, 1)
+    clean = amk.linear(x, *args)
+    last, t = width - 1, n - 1
+    for bad in ({3: math.inf}, {last: -math.inf}, {3: math.inf, last: math.inf}, {9: math.nan}):
+        odd = x.clone()
+        for k, value in bad.items():
+            odd[t, k] = value
+        y = amk.linear(odd, *args)
+        want = sum(value * w64[:, k] for k, value in bad.items())  # what is finite does not count beside it
+        assert torch.equal(torch.isnan(y[t]), torch.isnan(want))
+        assert torch.equal(y[t][torch.isinf(want)].double(), want[torch.isinf(want)])
+        assert torch.equal(y[:t], clean[:t])
+
+
+def test_infinite_scales(env):
+    """An infinite scale of the last group reaches its own row, also where the columns end inside a stage."""
+    amk, torch = env
+    for n, width, out, group in TILES:
+        x = randn(torch, n, n, width).to(torch.bfloat16)
+        c, s = codes_and_scale(torch, 6, 1, 7, out, width, group)
+        x[:, -group:] = x[:, -group:].abs() + 1  # sums of the last group are positive
+        clean = amk.linear(x, packed(torch, c), s, "w4a16", group)
+        s[out // 2, -1] = math.inf
+        y = amk.linear(x, packed(torch, c), s, "w4a16", group)
+        rest = [r for r in range(out) if r != out // 2]
+        assert (y[:, out // 2] == math.inf).all() and torch.equal(y[:, rest], clean[:, rest])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "w8a16", "w4a16"])
+@pytest.mark.parametrize("n", [17, 32, 33, 64, 100, 127])
+@pytest.mark.parametrize("out", [32700, 128256])
+def test_few_tokens_by_many_rows(env, fmt, n, out):
+    """The logits of a drafted tree: tiles of more tokens than there are."""
+    amk, torch = env
+    width, group = 352, 32
+    x = randn(torch, n, n, width).to(torch.bfloat16)
+    c, s = codes_and_scale(torch, 7, -8, 7, out, width, group)
+    if fmt == "bf16":
+        y, w = amk.linear(x, c.to(torch.bfloat16)), c.float()
+    elif fmt == "w8a16":
+        one = s[:, 0].float().contiguous()
+        y, w = amk.linear(x, c.to(torch.int8), one, fmt), c.float() * one[:, None]
+    else:
+        y, w = amk.linear(x, packed(torch, c), s, fmt, group), c.float() * s.float().repeat_interleave(group, 1)
+    w = w.double()
+    tol = (width + 4) * 2.0 ** -24 * (x.double().abs() @ w.abs().t())
+    assert float(((y.double() - x.double() @ w.t()).abs() - tol).max()) <= 0
 
 
 # ---- attention -----------------------------------------------------------------------------
