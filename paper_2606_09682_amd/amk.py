@@ -316,6 +316,10 @@ def _int32(value: int, what: str) -> None:
         raise ValueError(f"{what} = {value} does not fit 32 bits")
 
 
+def _past_int32(*sizes: int):
+    raise ValueError(f"a size of {max(sizes)} does not fit 32 bits")
+
+
 def _device_index(t, what: str) -> int:
     index = t.get_device()
     if index < 0:
@@ -345,7 +349,9 @@ def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, o
         _refuse(w, "w", index, _WEIGHT[fmt], 2)
     n, width = x.shape
     rows, stored = w.shape
-    _int32(n, "n"), _int32(rows, "w's rows"), _int32(group_size, "group_size")
+    if (n | width | rows) >> 31:
+        _past_int32(n, width, rows)
+    _int32(group_size, "group_size")
     if n and x.stride(1) != 1:
         raise ValueError("x must have contiguous rows")
     if (stored * 2 if fmt == AMK_WEIGHTS_W4A16 else stored) != width or not w.is_contiguous():
@@ -400,6 +406,9 @@ def _attention(q, k, v, scale, out):
     if v.get_device() != index or v.dtype not in _BF16 or v.dim() != 3:
         _refuse(v, "v", index, _BF16, 3)
     tokens, heads, d = q.shape
+    rows, kv_heads, _ = k.shape
+    if (tokens | heads | d | rows | kv_heads) >> 31:
+        _past_int32(tokens, heads, d, rows, kv_heads)
     if k.shape != v.shape or k.shape[2] != d:
         raise ValueError("k and v must be [rows, kv heads, head_dim] with q's head_dim")
     if out is None:
@@ -410,7 +419,7 @@ def _attention(q, k, v, scale, out):
         if out.shape != q.shape:
             raise ValueError("out must have q's shape")
     a = amk_attention_t(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *_strides(q, "q"), *_strides(k, "k"),
-                        *_strides(v, "v"), *_strides(out, "out"), heads, k.shape[1], d,
+                        *_strides(v, "v"), *_strides(out, "out"), heads, kv_heads, d,
                         d ** -0.5 if scale is None else scale)
     return a, out, index
 
@@ -432,6 +441,7 @@ def prompt_attention(q, k, v, cu_q=None, cu_k=None, scale: Optional[float] = Non
             if not t.is_contiguous() or t.numel() != cu_q.numel() or t.numel() < 1:
                 raise ValueError("cu_q and cu_k must be contiguous and of one length")
         seqs, pq, pk = cu_q.numel() - 1, cu_q.data_ptr(), cu_k.data_ptr()
+        _int32(seqs, "the number of sequences")
     lib = load()
     tokens, rows = q.shape[0], k.shape[0]
     need = lib.amk_prompt_attention_workspace(a.n_heads, a.n_kv_heads, a.head_dim, seqs, tokens, rows)
@@ -481,7 +491,8 @@ def token_logprobs(logits, tokens=None, top: int = 0):
     if kind is None or logits.dim() != 2:
         _refuse(logits, "logits", index, tuple(_LOGITS), 2)
     n, vocab = logits.shape
-    _int32(n, "n"), _int32(vocab, "vocab")
+    if (n | vocab) >> 31:
+        _past_int32(n, vocab)
     if n and vocab > 1 and logits.stride(1) != 1:
         raise ValueError("logits must have contiguous rows")
     if not 0 <= top <= AMK_TOP_MAX:
@@ -518,7 +529,9 @@ def kv_keep(kv, pos: int, rows) -> None:
         raise ValueError("kv must be a contiguous bf16 tensor [layers, 2, kv heads, max_seq, head_dim]")
     layers, _, heads, cap, d = kv.shape
     n = len(rows)
-    _int32(pos, "pos"), _int32(cap, "max_seq")
+    _int32(pos, "pos")
+    if (layers | heads | cap | d) >> 31:
+        _past_int32(layers, heads, cap, d)
     if n:
         _int32(min(rows), "a row"), _int32(max(rows), "a row")
     _call(index, load().amk_kv_keep, kv.data_ptr(), layers, heads, cap, d, pos, (ctypes.c_int32 * n)(*rows), n)

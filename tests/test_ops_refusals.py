@@ -1,0 +1,80 @@
+"""What the operators for several tokens refuse before anything is launched or allocated: sizes past 32 bits in the
+binding (no GPU)."""
+import os
+
+import pytest
+import torch
+
+from paper_2606_09682_amd import amk
+
+P = 4096  # a 256-byte aligned address that is never followed
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(amk.LIB_PATH):
+        from paper_2606_09682_amd import build
+        build.build()
+    return amk.load()
+
+
+class View:
+    """What the binding asks of a device tensor, of a shape that would not fit this machine."""
+    device = torch.device("cuda", 0)
+
+    def __init__(self, *shape, dtype=torch.bfloat16):
+        self.shape, self.dtype = shape, dtype
+
+    def get_device(self):
+        return 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        n = 1
+        for s in self.shape:
+            n *= s
+        return n
+
+    def stride(self, i=None):
+        strides = [1]
+        for s in self.shape[:0:-1]:
+            strides.insert(0, strides[0] * s)
+        return tuple(strides) if i is None else strides[i]
+
+    def is_contiguous(self):
+        return True
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def data_ptr(self):
+        return P
+
+
+BIG = (1 << 32) + 64  # 64 if cut to 32 bits
+
+
+@pytest.mark.parametrize("call", [
+    lambda: amk.linear(View(BIG, 64), View(64, 64)),
+    lambda: amk.linear(View(1, BIG), View(64, BIG)),
+    lambda: amk.linear(View(1, 64), View(BIG, 64)),
+    lambda: amk.prompt_attention(View(BIG, 4, 64), View(9, 4, 64), View(9, 4, 64), out=View(BIG, 4, 64)),
+    lambda: amk.prompt_attention(View(9, BIG, 64), View(9, 4, 64), View(9, 4, 64), out=View(9, BIG, 64)),
+    lambda: amk.prompt_attention(View(9, 4, BIG), View(9, 4, BIG), View(9, 4, BIG), out=View(9, 4, BIG)),
+    lambda: amk.prompt_attention(View(9, 4, 64), View(BIG, 4, 64), View(BIG, 4, 64), out=View(9, 4, 64)),
+    lambda: amk.prompt_attention(View(9, BIG, 64), View(9, BIG, 64), View(9, BIG, 64), out=View(9, BIG, 64)),
+    lambda: amk.prompt_attention(View(9, 4, 64), View(9, 4, 64), View(9, 4, 64), View(BIG, dtype=torch.int32),
+                                 View(BIG, dtype=torch.int32), out=View(9, 4, 64)),
+    lambda: amk.tree_attention(View(1, 4, 64), View(BIG, 4, 64), View(BIG, 4, 64), 1 << 32, [1], out=View(1, 4, 64)),
+    lambda: amk.token_logprobs(View(BIG, 100, dtype=torch.float32)),
+    lambda: amk.token_logprobs(View(1, BIG, dtype=torch.float32)),
+    lambda: amk.kv_keep(View(BIG, 2, 4, 100, 64), 0, [1]),
+    lambda: amk.kv_keep(View(4, 2, BIG, 100, 64), 0, [1]),
+    lambda: amk.kv_keep(View(4, 2, 4, BIG, 64), 0, [1]),
+    lambda: amk.kv_keep(View(4, 2, 4, 100, BIG), 0, [1]),
+])
+def test_sizes_past_32_bits(lib, call):
+    with pytest.raises(ValueError, match="does not fit 32 bits"):
+        call()
