@@ -34,6 +34,10 @@ bool shape_ok(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t tot
          total_q * n_heads <= kMostRows && keys <= kMostRows;
 }
 
+bool grid_ok(const AttnPlan& p, int32_t n_kv_heads) {
+  return (int64_t)p.tiles * p.splits * n_kv_heads <= kMostThreads / (64 * p.waves);
+}
+
 int check_workspace(const void* p, size_t have, size_t need) {
   if (need == 0) return AMK_OK;
   return p && aligned(p, 256) && have >= need ? AMK_OK : AMK_ERR_INVALID_ARGUMENT;
@@ -82,7 +86,7 @@ int amk_prompt_attention(const amk_attention_t* a, const int32_t* cu_q, const in
   int st = check_attention(a, total_q, total_k);
   if (st != AMK_OK) return st;
   const AttnPlan p = prompt_plan(a->n_heads, a->n_kv_heads, a->head_dim, n_seqs, total_q, total_k);
-  if ((int64_t)p.tiles * p.splits * a->n_kv_heads > kMostThreads / (64 * p.waves)) return AMK_ERR_UNSUPPORTED;
+  if (!grid_ok(p, a->n_kv_heads)) return AMK_ERR_UNSUPPORTED;
   st = check_workspace(workspace, workspace_bytes, p.workspace);
   if (st != AMK_OK) return st;
   return launch_prompt(*a, p, cu_q, cu_k, n_seqs, total_q, total_k, workspace, stream);
@@ -101,6 +105,7 @@ int amk_tree_attention(const amk_attention_t* a, int32_t n, int32_t pos, const u
   int st = check_attention(a, n, (int64_t)pos + n);
   if (st != AMK_OK) return st;
   const AttnPlan p = tree_plan(a->n_heads, a->n_kv_heads, a->head_dim, n, pos);
+  if (!grid_ok(p, a->n_kv_heads)) return AMK_ERR_UNSUPPORTED;
   st = check_workspace(workspace, workspace_bytes, p.workspace);
   if (st != AMK_OK) return st;
   TreeMasks m = {};

@@ -1,5 +1,6 @@
 """What the operators for several tokens refuse before anything is launched or allocated: sizes past 32 bits in the
-binding (no GPU)."""
+binding, grids past the hardware's limit (no GPU)."""
+import ctypes
 import os
 
 import pytest
@@ -78,3 +79,11 @@ BIG = (1 << 32) + 64  # 64 if cut to 32 bits
 def test_sizes_past_32_bits(lib, call):
     with pytest.raises(ValueError, match="does not fit 32 bits"):
         call()
+
+
+@pytest.mark.parametrize("n,heads", [(1, 1 << 30), (8, 1 << 27)])
+def test_tree_grid_past_the_limit(lib, n, heads):
+    """A workgroup at least for every KV head, below 2^32 threads in all."""
+    a = amk.amk_attention_t(P, P, P, P, 64, 64, 64, 64, 64, 64, 64, 64, heads, heads, 64, 1.0)
+    masks = (ctypes.c_uint64 * n)(*[1] * n)
+    assert lib.amk_tree_attention(a, n, 5, masks, None, 0, None) == amk.AMK_ERR_UNSUPPORTED
