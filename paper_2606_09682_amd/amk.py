@@ -704,10 +704,19 @@ class Decoder:
     def score(self, tokens, pos: int, kv_cache, top: int = 0):
         """Score a text behind the `pos` positions in the cache: (logprob, entropy,
         top_ids, top_logprobs) of tokens[1:], each given those before it
-        (token_logprobs over extend's logits).  Appends the rows of all its tokens."""
+        (token_logprobs over extend's logits).  Appends the rows of all its tokens.  The
+        tokens are copied to the device, which waits for what its stream has queued: not for
+        graphs."""
         import torch
         if len(tokens) < 2:
             raise ValueError("a text to score has at least two tokens")
+        # a long text is taken in pieces: nothing runs before all of it is found good
+        if not 0 <= top <= min(AMK_TOP_MAX, self.cfg.vocab):
+            raise ValueError(f"top must be in [0, {min(AMK_TOP_MAX, self.cfg.vocab)}]")
+        least, most = min(tokens), max(tokens)
+        _int32(least, "a token"), _int32(most, "a token")
+        if least < 0 or most >= self.cfg.vocab:
+            raise AmkError(AMK_ERR_INVALID_ARGUMENT, "amk_extend")
         if pos + len(tokens) > self.cfg.max_seq:
             raise ValueError(f"{len(tokens)} tokens at {pos} exceed the cache's {self.cfg.max_seq} positions")
         parts = []

@@ -1,5 +1,5 @@
 """What the operators for several tokens refuse before anything is launched or allocated: sizes past 32 bits in the
-binding, grids past the hardware's limit (no GPU)."""
+binding, grids past the hardware's limit, texts that a later piece would refuse (no GPU)."""
 import ctypes
 import os
 
@@ -87,3 +87,17 @@ def test_tree_grid_past_the_limit(lib, n, heads):
     a = amk.amk_attention_t(P, P, P, P, 64, 64, 64, 64, 64, 64, 64, 64, heads, heads, 64, 1.0)
     masks = (ctypes.c_uint64 * n)(*[1] * n)
     assert lib.amk_tree_attention(a, n, 5, masks, None, 0, None) == amk.AMK_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("tokens,top,error", [
+    ([1] * 3000, 33, ValueError), ([1] * 3000, -1, ValueError), ([1] * 2999 + [100], 3, amk.AmkError),
+    ([1] * 2999 + [-1], 3, amk.AmkError), ([1] * 2999 + [1 << 32], 3, ValueError), ([1], 3, ValueError),
+    ([1] * 5000, 3, ValueError), ([1, 100], 0, amk.AmkError), ([1, 2], 33, ValueError)])
+def test_score_refuses_before_it_runs(lib, tokens, top, error):
+    """A text is taken in pieces: one that cannot be scored whole leaves the cache as it was."""
+    dec = object.__new__(amk.Decoder)
+    dec.handle = None
+    dec.cfg = amk.make_config(64, 1, 1, 1, 64, 64, 100, 4096, 1e4)
+    dec.extend = lambda *a, **k: pytest.fail("a piece was run")
+    with pytest.raises(error):
+        dec.score(tokens, 0, torch.zeros(1), top)
