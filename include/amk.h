@@ -302,7 +302,9 @@ int amk_read_probe(const void* buf, int64_t bytes, int32_t blocks, uint32_t* sin
  * NULL or misaligned pointer, a size or stride out of range or a workspace too
  * small, AMK_ERR_UNSUPPORTED for a shape outside the family, AMK_ERR_DEVICE for
  * a failed launch.  Results do not depend on the order in which work happens to
- * run: the same call gives the same bits. */
+ * run: the same call gives the same bits.  How many tokens share a call decides the
+ * order in which a product or an attention adds up, so a token's bits may differ
+ * between calls of different sizes, by the roundings of that order. */
 
 /* Element types of operators that take several. */
 enum { AMK_F32 = 0, AMK_BF16 = 1, AMK_F16 = 2 };
@@ -331,9 +333,9 @@ int amk_linear(const void* x, int64_t x_stride, int32_t n, int32_t in, int32_t o
  * and 2^30 pairs of a token and a query head.
  * Scores, softmax statistics and the weighted sums are fp32; weights are
  * rounded to bf16 for the product with v.  A key scoring minus infinity counts as
- * not seen, and a row that sees no key gets zeros; what a row does not see never
- * reaches it, not even its last bit, infinities and NaN included.  An infinity or
- * NaN in v reaches every row that sees its key, however small the weight. */
+ * not seen, and a row that sees no key gets zeros; the values that a row does not
+ * see never reach it, not even its last bit, infinities and NaN included.  An infinity
+ * or NaN in v reaches every row that sees its key, however small the weight. */
 typedef struct {
   const void* q;
   const void* k;

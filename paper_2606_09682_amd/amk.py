@@ -271,7 +271,9 @@ def amk_schedule_check(cfg: amk_config_t, n_cu: int, tasks, n_counters: int,
 # outputs and workspaces are allocated too; nothing synchronises.  The library sees
 # bare pointers, so types, shapes, devices and strides are checked here.  Small calls
 # take the GPU a few microseconds, so what runs on every call is kept short: a stream
-# is read as its raw handle, and messages are made only for a refusal.
+# is read as its raw handle, and messages are made only for a refusal.  They serve
+# inference: results have no gradients, whether or not an operand requires them, and
+# autograd does not see what is written to `out` or a cache.
 _SCORE_CHUNK = 2048  # tokens whose logits Decoder.score holds at once: what amk_extend takes through the model at once
 _FORMATS = {"bf16": AMK_WEIGHTS_BF16, "w8a16": AMK_WEIGHTS_W8A16, "w4a16": AMK_WEIGHTS_W4A16}
 _torch = None
@@ -333,7 +335,7 @@ def _workspace(nbytes: int, index: int):
 
 def linear(x, w, scale=None, weight_format: str = "bf16", group_size: int = 0, out=None, out_dtype=None,
            accumulate: bool = False):
-    """x W^T for n tokens (amk_linear): x bf16 [n, in] with contiguous rows; w and
+    """x W^T for n tokens (amk_linear; no gradients): x bf16 [n, in] with contiguous rows; w and
     scale a projection as Decoder takes it ([out, in] bf16 or int16 bits; int8 with
     fp32 scale [out]; packed uint8 [out, in / 2] with fp16 scale [out, in / group]).
     Returns [n, out] of out_dtype (fp32, the default, or bf16), or writes it to `out`
@@ -425,11 +427,12 @@ def _attention(q, k, v, scale, out):
 
 
 def prompt_attention(q, k, v, cu_q=None, cu_k=None, scale: Optional[float] = None, out=None):
-    """Causal attention over whole prompts (amk_prompt_attention): q bf16 [tokens,
-    heads, head_dim], k and v [rows, kv heads, head_dim], any strides with contiguous
+    """Causal attention over whole prompts (amk_prompt_attention; no gradients): q bf16
+    [tokens, heads, head_dim], k and v [rows, kv heads, head_dim], any strides with contiguous
     heads (a cache layer kv[l, 0] is taken as kv[l, 0].transpose(0, 1)).  cu_q and
     cu_k: int32 device tensors [sequences + 1] of offsets, or both None for one
-    sequence.  Rows of `out` outside every sequence are not written."""
+    sequence.  Rows of `out` outside every sequence are not written; without `out` they
+    hold whatever the memory did."""
     a, out, index = _attention(q, k, v, scale, out)
     seqs, pq, pk = 1, None, None
     if (cu_q is None) != (cu_k is None):
@@ -462,8 +465,8 @@ def tree_masks(parents):
 
 
 def tree_attention(q, k, v, pos: int, masks, scale: Optional[float] = None, out=None):
-    """Attention of n drafted tokens over a cache (amk_tree_attention): q bf16 [n,
-    heads, head_dim]; k and v [rows, kv heads, head_dim] as in prompt_attention, with
+    """Attention of n drafted tokens over a cache (amk_tree_attention; no gradients): q
+    bf16 [n, heads, head_dim]; k and v [rows, kv heads, head_dim] as in prompt_attention, with
     at least pos + n rows; masks: n whole numbers, bit j of masks[i] set where token
     i sees row pos + j (tree_masks gives a tree's)."""
     a, out, index = _attention(q, k, v, scale, out)
@@ -482,8 +485,8 @@ def tree_attention(q, k, v, pos: int, masks, scale: Optional[float] = None, out=
 
 
 def token_logprobs(logits, tokens=None, top: int = 0):
-    """(logprob, entropy, top_ids, top_logprobs) of rows of logits (amk_token_logprobs):
-    logits fp32, bf16 or fp16 [n, vocab] with contiguous rows; tokens int32 [n], or
+    """(logprob, entropy, top_ids, top_logprobs) of rows of logits (amk_token_logprobs; no
+    gradients): logits fp32, bf16 or fp16 [n, vocab] with contiguous rows; tokens int32 [n], or
     None (logprob is then None); the `top` most probable tokens of each row."""
     torch = _torch or _load_torch()
     index = _device_index(logits, "logits")

@@ -39,9 +39,9 @@
 // of the time and no LDS read meets another's bank: 535 us, 1030 TFLOP/s (a large bf16
 // product reaches 1380).  Heads of 64 do half the products for the same softmax: six
 // packed sequences of 4092 tokens, 32 and 4 heads, 50 us, 610 TFLOP/s.  64 drafted tokens
-// at position 32001, 32 and 8 heads of 128, take 46 us and 9 more to join 32 splits (33
-// MB of partial sums): 2.4 TB/s, where both the keys and the products have a floor of 24.
-// Eight tokens at 300, 9 and 3 heads of 64, take 8.5 us, ten tiles one after another.
+// at position 32001, 32 and 8 heads of 128, take 46 us and 8 more to join 32 splits (33
+// MB of partial sums): 2.5 TB/s, where both the keys and the products have a floor of 24.
+// Eight tokens at 300, 9 and 3 heads of 64, take 8.1 us, ten tiles one after another.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -565,14 +565,19 @@ AttnPlan with_workspace(AttnPlan p, int n_heads, int head_dim, int total_q) {
   return p;
 }
 
-// Workgroups that run at once: each CU has registers for 8 waves.
+// Workgroups a plan with splits may launch: eight waves a CU, two per SIMD.  That is what
+// runs at once for heads of 128 in workgroups of 2 waves and more.  Workgroups of one wave have
+// LDS for four a CU, so the longest contexts of a few tokens take two rounds; heads of 64
+// would leave room for 9 to 12 waves.
 int resident(int waves) { return 256 * 8 / waves; }
 
 // Waves (32 rows each) of a workgroup.  Eight share a tile of K and V among twice the rows
 // of four, but mask more at a causal diagonal, and `many` says that this pays: heads of 128,
-// us with eight / four waves: one prompt of 8192 tokens 523 / 540, two of 2048 82 / 87, eight
-// of 512 46 / 42; a tree of 64 tokens at 32001 54 / 59.  Heads of 64 gain nothing (a prompt
-// of 8192 330 / 318).
+// us with eight / four waves, 32 and 8 heads: one prompt of 8192 tokens 523 / 540, one of 4096
+// 148 / 161, two of 2048 85 / 90, two of 1800 71 / 72, three of 1400 79 / 72, four of 1024 66 / 59;
+// a tree of 64 tokens at 32001 54 / 59.  Prompts take eight from 8192 rows of a sequence on.
+// One KV head has too few tiles for it (8 and 1 heads, three of 1500 tokens 49 / 39).  Heads
+// of 64 gain nothing (a prompt of 8192 330 / 318).
 int waves_for(int64_t rows, int head_dim, bool many) {
   return rows <= 32 ? 1 : rows <= 64 ? 2 : many && head_dim == 128 ? 8 : 4;
 }
@@ -636,8 +641,11 @@ AttnPlan tree_plan(int n_heads, int n_kv_heads, int head_dim, int n, int pos) {
   const int64_t rows = (int64_t)n * (n_heads / n_kv_heads);
   p.waves = waves_for(rows, head_dim, rows > 128);
   p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  // Up to 320 keys one workgroup is done as soon as two and the join (8 tokens at 300, heads of
-  // 64: 8.4 us against 8.7); beyond, ranges of 128 keys (the same at 600: 11.8 us whole, 8.7).
+  // Up to 320 keys whole, beyond in ranges of 128, which need the join.  us whole / split of 8
+  // tokens, 9 and 3 heads of 64: 200 keys 6.7 / 8.4, 260 7.9 / 8.1, 320 8.3 / 8.4, 400 9.8 / 8.4;
+  // of 16, 32 and 4 heads of 64: 320 keys 8.7 / 9.3, 400 10.6 / 9.3.  The tiles of wider heads take
+  // longer, and pay from fewer keys on: 8 tokens, 32 and 8 heads of 128, 200 keys 10.2 / 10.6, 260
+  // 12.0 / 10.0, 320 12.7 / 10.7.
   const int64_t keys = (int64_t)pos + n;
   p.splits = keys <= 320 ? 1 : splits_for((int64_t)p.tiles * n_kv_heads, p.waves, keys, 128);
   return with_workspace(p, n_heads, head_dim, n);

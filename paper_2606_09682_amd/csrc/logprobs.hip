@@ -9,8 +9,9 @@
 // instructions an entry) bound large calls and the two launches small ones.
 // Chunks of 8192 entries are few for the join and leave registers for six waves
 // per SIMD: 1024 x 128256 fp32 logits with 20 alternatives take 99 us (5.3 TB/s),
-// with five waves 106; bf16 104.  Quarter chunks for few rows only make the join
-// longer: one row 12.6 us and 16 rows 30.5, not 8.8 and 13.9.
+// with five waves 106; bf16 104.  (At six, one register of the fp32 kernel spills, 8 bytes a
+// lane.)  Quarter chunks for few rows only make the join longer: one row 12.6 us and 16 rows
+// 30.5, not 8.8 and 13.9.
 //
 // Best entries.  Each lane's maximum over the workgroup's waves gives 64 maxima
 // of disjoint groups; the top-th largest of them is a value that at least `top`
