@@ -18,7 +18,10 @@
 // 0..7 of lane half h stand for keys 4h..4h+3 and 8+4h..8+4h+3 of each 16: V^T's
 // operand is read from the row-major tile in exactly that order by the
 // transposed LDS reads.  P is rounded to bf16 (relative error at most 2^-8, of
-// the size of the output's own rounding); l sums the unrounded p in fp32.
+// the size of the output's own rounding); l sums the unrounded p in fp32.  Taking P's
+// remainder as a second operand brings an output's relative error from 0.0021 to 0.0017,
+// all but that of its own rounding, for half as many products again: a prompt of 8192
+// tokens 727 us, not 530, eight drafted tokens at 300 9.6, not 8.1.
 //
 // LDS.  K and V tiles are loaded straight to LDS (16 bytes a lane), two stages,
 // so a tile's loads run under the previous tile's products.  Rows lie without
